@@ -430,6 +430,99 @@ bd_status bd_linear_multitenant_tiled_group_q8(int32_t n_mats, const uint16_t* x
                                                int64_t T, const int64_t* out, int64_t in, int32_t n_tenants,
                                                void* stream);
 
+/* ---- low-rank adapters (the other kind of fine-tune that Sec. 4.3 compares with) ---------------------
+ * A tenant whose fine-tune is low rank brings, per matrix, A_e [r_e, in] and B_e [out, r_e], both fp16 row-major, and a scale s_e.
+ * These calls add what the adapters of ALL tokens of a batch give to what the shared projection gave, whichever of the linears
+ * above that was (an fp16 or 8-bit base, row-major or tiled, with or without 1-bit deltas):
+ *     h[t] = A_e x[t]                                  e = tenant_of_token[t]
+ *     y[t] = fp16( f32(y0[t]) + s_e * (B_e h[t]) )     one rounding; sums in binary32, h to 22 bits or more
+ *   x_f16            [T, in]
+ *   a_by_tenant, b_by_tenant   HOST arrays of n_tenants DEVICE pointers; NULL allowed for tenants without a token and where
+ *                    the rank is 0
+ *   rank_by_tenant   HOST [n_tenants], 0 .. BD_LORA_MAX_RANK each (checked for tenants with a token); 0: no adapter, y[t] = y0[t]
+ *   scale_by_tenant  device array of n_tenants floats
+ *   tenant_of_token  HOST [T], any order; tokens are grouped by tenant inside the call
+ *   y0_f16, y_f16    [T, out]; y0 may be NULL (zeros) or y itself, but not overlap y otherwise
+ *   h                NULL, or device [T, h_ld] floats that receive h[t][0 .. r_e) for the backward pass; h_ld >= the largest rank
+ *                    of the call's tokens; entries beyond a token's rank are left as they were
+ *   workspace        bd_lora_workspace_bytes(T, 1, largest rank) bytes, 256-byte aligned, device memory: holds h between the two
+ *                    launches (one call at a time per workspace; not needed where no token has an adapter)
+ * in % 32 == 0, out and in up to 2^24; T up to 65535, more than 64 tenants (16-token runs of tenants up to T = 512) run as several
+ * pairs of launches.  The sum over `in` is cut by a rule on the sizes of the call, so the last bits of h may change with the other
+ * tokens of the call.  No tensor that is written may overlap any other (BD_ERR_ALIAS). */
+#define BD_LORA_MAX_RANK 256
+size_t bd_lora_workspace_bytes(int64_t T, int32_t n_mats, int32_t max_rank);
+bd_status bd_lora_multitenant(const uint16_t* x_f16, const uint16_t* const* a_by_tenant, const uint16_t* const* b_by_tenant,
+                              const int32_t* rank_by_tenant, const float* scale_by_tenant, const int32_t* tenant_of_token,
+                              const uint16_t* y0_f16, uint16_t* y_f16, float* h, int32_t h_ld, int64_t T, int64_t out, int64_t in,
+                              int32_t n_tenants, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The adapters of up to 3 matrices that read the same x (q, k, v or gate, up) in the launches of one: HOST arrays as in
+ * bd_linear_multitenant_tiled_group, entry m * n_tenants + e (or m); y0_f16, h and their entries may be NULL.  The workspace is
+ * bd_lora_workspace_bytes(T, n_mats, largest rank). */
+bd_status bd_lora_multitenant_group(int32_t n_mats, const uint16_t* x_f16, const uint16_t* const* a_by_mat_tenant,
+                                    const uint16_t* const* b_by_mat_tenant, const int32_t* rank_by_mat_tenant,
+                                    const float* const* scale_by_mat, const int32_t* tenant_of_token, const uint16_t* const* y0_f16,
+                                    uint16_t* const* y_f16, float* const* h, int32_t h_ld, int64_t T, const int64_t* out, int64_t in,
+                                    int32_t n_tenants, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The gradients of bd_lora_multitenant, for training the adapters of several tenants at once:
+ *     g[t]  = s_e B_e^T dy[t]                       (binary32, to 22 bits or more where it is multiplied on)
+ *     dx[t] = fp16( f32(dx0[t]) + A_e^T g[t] )      dx0: the gradient through the shared projection, NULL (zeros) or dx itself
+ *     dA_e  = sum over e's tokens of g[t] x[t]^T    binary32 [r_e, in]
+ *     dB_e  = s_e * sum of dy[t] h[t]^T             binary32 [out, r_e]
+ *   dy_f16 [T, out]; x_f16 and h as of the forward call (h_ld too); the other arguments as there
+ *   dx_f16           [T, in], or NULL where it is not wanted
+ *   da_by_tenant, db_by_tenant   HOST arrays of n_tenants DEVICE pointers (16-byte aligned), NULL where a gradient is not wanted;
+ *                    either array may be NULL.  Inputs that no wanted result needs may be NULL.
+ *   accumulate       0: the gradients are overwritten, those of tenants without a token with zeros; else they are added to
+ *   workspace        bd_lora_backward_workspace_bytes(T, out, in, largest rank) bytes, 256-byte aligned, device memory
+ * Sums in binary32 in a fixed order: the same inputs give the same bits.  The ranks of tenants whose gradients are asked for are
+ * checked too.  Two tenants may share A and B, but not their gradients (BD_ERR_ALIAS). */
+size_t bd_lora_backward_workspace_bytes(int64_t T, int64_t out, int64_t in, int32_t max_rank);
+bd_status bd_lora_multitenant_backward(const uint16_t* dy_f16, const uint16_t* x_f16, const float* h, int32_t h_ld,
+                                       const uint16_t* const* a_by_tenant, const uint16_t* const* b_by_tenant,
+                                       const int32_t* rank_by_tenant, const float* scale_by_tenant, const int32_t* tenant_of_token,
+                                       const uint16_t* dx0_f16, uint16_t* dx_f16, float* const* da_by_tenant, float* const* db_by_tenant,
+                                       int32_t accumulate, int64_t T, int64_t out, int64_t in, int32_t n_tenants, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/* ---- AdamW over many tensors at once ------------------------------------------------------------------
+ * The step that fine-tunes come from: adapters (their gradients are those above, their fp16 copies what the calls above
+ * multiply by) or whole matrices (whose fp16 copy bd_compress takes).  Per element, in binary32:
+ *     g = grad * grad_scale;   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g g
+ *     p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps);   p_f16 = fp16(p)
+ * A PLAN holds the tensors' addresses and sizes, checked once: a block of bytes in HOST memory (8-byte aligned) that the caller
+ * owns and may copy; bd_adamw reads it while it enqueues and keeps nothing of it.
+ *   n                       tensors, up to BD_ADAMW_MAX_TENSORS; entries of HOST arrays of n DEVICE pointers below
+ *   param                   binary32, updated in place;  param_f16: their fp16 copies, written; the array or entries may be NULL
+ *   grad                    binary32, or fp16 where grad_f16 != 0
+ *   exp_avg, exp_avg_sq     m and v: binary32, or one byte per element where the two scale arrays are given
+ *   exp_avg_scale, exp_avg_sq_scale   NULL, or one float per block of 256 elements of a tensor (its last block may be shorter)
+ *   numel                   HOST [n], 0 .. BD_ADAMW_MAX_ELEMENTS; a tensor of none is skipped
+ * Tensors 16-byte aligned, scales 4.  Nothing may overlap anything else (BD_ERR_ALIAS): no tensor twice.
+ * States in 8 bits: a byte's value is V times its block's scale, V = f where the exponent bits e are 0, else (2^F + f) 2^(e-1).
+ *     m: bit 7 the sign, bits 6-4 e, bits 3-0 f (F = 4); m = +-scale V, rounded to nearest even; scale = max |m| / 1984
+ *     v: bits 7-5 e, bits 4-0 f (F = 5); sqrt(v) = scale V; scale = sqrt(max v) / 4032; rounded up with the probability of its
+ *        fraction of a code step, by a hash of (index in the tensor, step), never to zero where v is not
+ *   The update itself uses m and v before they are rounded.  All zeros (bytes and scales) is the state before the first step.  A
+ *   block with an infinity or NaN becomes NaN; one whose largest |m| is below 2^-100 becomes zero.
+ * bd_adamw:
+ *   lr, step                device, one float and one int64: the learning rate and the number t >= 1 of this step (read when
+ *                           the kernel runs, so that a captured step can be replayed with the next ones)
+ *   grad_scale              device, one float, or NULL (1): what undoes a loss scale, or clips
+ *   skip                    device, one int32, or NULL: not 0 leaves everything as it was (a step whose gradients overflowed)
+ *   beta1, beta2 in [0, 1), eps, weight_decay >= 0, else BD_ERR_UNSUPPORTED.  BD_ERR_FORMAT: not a plan.
+ * 40 tensors per launch. */
+#define BD_ADAMW_MAX_TENSORS 1048576
+#define BD_ADAMW_MAX_ELEMENTS ((int64_t)1 << 35)
+size_t bd_adamw_plan_bytes(int32_t n);
+bd_status bd_adamw_plan(void* plan, size_t plan_bytes, int32_t n, float* const* param, uint16_t* const* param_f16, const void* const* grad,
+                        int32_t grad_f16, void* const* exp_avg, void* const* exp_avg_sq, float* const* exp_avg_scale,
+                        float* const* exp_avg_sq_scale, const int64_t* numel);
+bd_status bd_adamw(const void* plan, size_t plan_bytes, const float* lr, const int64_t* step, const float* grad_scale, const int32_t* skip,
+                   double beta1, double beta2, double eps, double weight_decay, void* stream);
+
 /* ---- delta images: storing a tenant's delta and swapping it in while serving ----------------
  * Sec. 3.3 of the paper: a 1-bit delta is small enough to be kept per tenant on disk or in host
  * memory and loaded on demand.  A delta IMAGE holds one tenant's whole compressed model (every

@@ -34,7 +34,8 @@ EXPORTS = ["bd_status_string", "bd_version", "bd_workspace_bytes", "bd_pack_sign
            "bd_compress_q8", "bd_tiled_base_q8_bytes", "bd_tile_base_q8", "bd_linear_multitenant_tiled_q8",
            "bd_linear_multitenant_tiled_group_q8", "bd_linear_multitenant_kbit", "bd_linear_multitenant_gemm_kbit",
            "bd_linear_multitenant_gemm_q8", "bd_linear_multitenant_q8", "bd_linear_multitenant_gemm_kbit_variant",
-           "bd_linear_multitenant_gemm_q8_variant"]
+           "bd_linear_multitenant_gemm_q8_variant", "bd_lora_workspace_bytes", "bd_lora_multitenant", "bd_lora_multitenant_group",
+           "bd_lora_backward_workspace_bytes", "bd_lora_multitenant_backward", "bd_adamw_plan_bytes", "bd_adamw_plan", "bd_adamw"]
 
 
 class BitDeltaError(RuntimeError):
@@ -116,6 +117,18 @@ def lib() -> ctypes.CDLL:
         L.bd_compress_batch.restype = ctypes.c_int
         L.bd_linear_multitenant_tiled_kbit.argtypes = [vp, vp, pvp, vp, pi, vp, i64, i64, i64, i32, i32, vp]
         L.bd_linear_multitenant_tiled_group_kbit.argtypes = [i32, vp, pvp, pvp, pvp, pi, pvp, i64, pi64, i64, i32, i32, vp]
+        L.bd_lora_workspace_bytes.restype = sz
+        L.bd_lora_workspace_bytes.argtypes = [i64, i32, i32]
+        L.bd_lora_multitenant.argtypes = [vp, pvp, pvp, pi, vp, vp, vp, vp, vp, i32, i64, i64, i64, i32, vp, sz, vp]
+        L.bd_lora_multitenant_group.argtypes = [i32, vp, pvp, pvp, pi, pvp, vp, pvp, pvp, pvp, i32, i64, pi64, i64, i32, vp, sz, vp]
+        L.bd_lora_backward_workspace_bytes.restype = sz
+        L.bd_lora_backward_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.bd_lora_multitenant_backward.argtypes = [vp, vp, vp, i32, pvp, pvp, pi, vp, vp, vp, vp, pvp, pvp, i32, i64, i64, i64, i32, vp, sz, vp]
+        L.bd_adamw_plan_bytes.restype = sz
+        L.bd_adamw_plan_bytes.argtypes = [i32]
+        L.bd_adamw_plan.argtypes = [vp, sz, i32, pvp, pvp, pvp, i32, pvp, pvp, pvp, pvp, pi64]
+        dbl = ctypes.c_double
+        L.bd_adamw.argtypes = [vp, sz, vp, vp, vp, vp, dbl, dbl, dbl, dbl, vp]
         for name in ("bd_pack_signs", "bd_compress", "bd_linear_multitenant", "bd_linear_multitenant_variant",
                      "bd_materialize", "bd_linear_naive", "bd_probe_read", "bd_probe_copy", "bd_tile_base",
                      "bd_tile_signs", "bd_linear_multitenant_tiled", "bd_linear_multitenant_tiled_group"):
@@ -856,3 +869,283 @@ def linear_multitenant_tiled_group_q8(x: torch.Tensor, group: TiledGroup, tenant
                                                       group.out_arr, inn, group.n_tenants, _stream(stream)),
            "bd_linear_multitenant_tiled_group_q8")
     return list(ys)
+
+
+# ---- low-rank adapters -----------------------------------------------------------------------------------
+
+LORA_MAX_RANK = 256
+
+
+def _here(*tensors) -> None:
+    """The tensors of a call are on the current device: its kernels run there."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def _tok_pointer(tenant_of_token, T: int):
+    """The tokens' tenants as the library takes them, and what keeps them alive: a CPU int32 tensor is passed as it is."""
+    if isinstance(tenant_of_token, torch.Tensor):
+        t = tenant_of_token
+        if t.device.type != "cpu" or t.dtype != torch.int32 or not t.is_contiguous():
+            raise TypeError("tenant_of_token: a sequence of ints or a contiguous int32 CPU tensor")
+        n, keep, p = t.numel(), t, t.data_ptr()
+    else:
+        n, keep = len(tenant_of_token), _tok_array(tenant_of_token)
+        p = ctypes.addressof(keep)
+    if n != T:
+        raise ValueError("one tenant per token")
+    return p, keep
+
+
+def lora_workspace_bytes(T: int, n_mats: int, max_rank: int) -> int:
+    return int(lib().bd_lora_workspace_bytes(T, n_mats, max_rank))
+
+
+def lora_backward_workspace_bytes(T: int, out: int, inn: int, max_rank: int) -> int:
+    return int(lib().bd_lora_backward_workspace_bytes(T, out, inn, max_rank))
+
+
+class LoraTable:
+    """The adapters of one matrix: HOST arrays of device pointers to every tenant's A [r, in] and B [out, r] (fp16; None = the
+    tenant has no adapter) and of ranks, and the device array of scales."""
+
+    def __init__(self, a_by_tenant: Sequence[Optional[torch.Tensor]], b_by_tenant: Sequence[Optional[torch.Tensor]], scale_by_tenant):
+        self.a, self.b = list(a_by_tenant), list(b_by_tenant)
+        if len(self.a) != len(self.b):
+            raise ValueError("one A and one B per tenant")
+        shapes = set()
+        for a, b in zip(self.a, self.b):
+            if (a is None) != (b is None):
+                raise ValueError("an adapter is A and B")
+            if a is not None:
+                _dev(a, torch.float16, "A")
+                _dev(b, torch.float16, "B")
+                if a.dim() != 2 or b.dim() != 2 or a.shape[0] != b.shape[1]:
+                    raise ValueError("A is [r, in] and B [out, r]")
+                shapes.add((b.shape[0], a.shape[1]))
+        if len(shapes) > 1:
+            raise ValueError("the adapters of one matrix have the same out and in")
+        self.shape = shapes.pop() if shapes else None   # (out, in)
+        self.ranks = [0 if a is None else int(a.shape[0]) for a in self.a]
+        self.max_rank = max(self.ranks, default=0)
+        n = max(len(self.a), 1)
+        self.a_ptrs = (ctypes.c_void_p * n)(*[_ptr(a) or None for a in self.a])
+        self.b_ptrs = (ctypes.c_void_p * n)(*[_ptr(b) or None for b in self.b])
+        self.rank_arr = (ctypes.c_int32 * n)(*self.ranks)
+        dev = next((a.device for a in self.a if a is not None), torch.device("cuda"))
+        if isinstance(scale_by_tenant, torch.Tensor):
+            self.scale = scale_by_tenant.to(device=dev, dtype=torch.float32).reshape(-1).contiguous()
+        else:
+            self.scale = torch.tensor([float(s) for s in scale_by_tenant], dtype=torch.float32, device=dev)
+        if self.scale.numel() != len(self.a):
+            raise ValueError("one scale per tenant")
+
+    @property
+    def n_tenants(self) -> int:
+        return len(self.a)
+
+
+class LoraGroup:
+    """Marshalled arguments of bd_lora_multitenant_group for a fixed set of matrices."""
+
+    def __init__(self, tables: Sequence[LoraTable], outs: Sequence[int]):
+        self.tables, self.outs, self.n = list(tables), [int(o) for o in outs], len(tables)
+        if self.n < 1 or len(self.outs) != self.n or any(t.n_tenants != tables[0].n_tenants for t in tables):
+            raise ValueError("every matrix needs the same tenants, and its number of outputs")
+        if any(t.shape is not None and t.shape[0] != o for t, o in zip(self.tables, self.outs)):
+            raise ValueError("an adapter's out is not its matrix's")
+        if len({t.shape[1] for t in self.tables if t.shape is not None}) > 1:
+            raise ValueError("the matrices of a group read the same x")
+        self.n_tenants = tables[0].n_tenants
+        self.inn = next((t.shape[1] for t in self.tables if t.shape is not None), None)
+        self.max_rank = max(t.max_rank for t in self.tables)
+        flat = lambda get: [v for t in self.tables for v in list(get(t))[:self.n_tenants]]
+        size = max(self.n * self.n_tenants, 1)
+        self.a_ptrs = (ctypes.c_void_p * size)(*flat(lambda t: t.a_ptrs))
+        self.b_ptrs = (ctypes.c_void_p * size)(*flat(lambda t: t.b_ptrs))
+        self.rank_arr = (ctypes.c_int32 * size)(*flat(lambda t: t.rank_arr))
+        self.scale = (ctypes.c_void_p * self.n)(*[_ptr(t.scale) or None for t in self.tables])
+        self.out_arr = (ctypes.c_int64 * self.n)(*self.outs)
+
+
+def _lora_rows(t: Optional[torch.Tensor], T: int, width: int, what: str) -> None:
+    if t is not None:
+        _dev(t, torch.float16, what)
+        if tuple(t.shape) != (T, width):
+            raise ValueError(f"{what} must be [{T}, {width}]")
+
+
+def _lora_h(h: Optional[torch.Tensor], T: int) -> int:
+    if h is None:
+        return 0
+    _dev(h, torch.float32, "h")
+    if h.dim() != 2 or h.shape[0] != T:
+        raise ValueError(f"h must be [{T}, at least the largest rank]")
+    return int(h.shape[1])
+
+
+def lora_multitenant(x: torch.Tensor, adapters: LoraTable, tenant_of_token, y0: Optional[torch.Tensor] = None,
+                     y: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     stream=None, out: Optional[int] = None) -> torch.Tensor:
+    """bd_lora_multitenant: y fp16 [T, out] = y0 + what every token's adapter adds.  y0: what the shared projection gave (None: zeros;
+    y=y0: in place).  h: float32 [T, >= largest rank] that receives A x for the backward pass.  tenant_of_token: a sequence, or a CPU
+    int32 tensor (no conversion).  out: needed only where no tenant has an adapter and neither y0 nor y is given."""
+    _dev(x, torch.float16, "x")
+    T, inn = x.shape
+    out = next((int(t.shape[1]) for t in (y, y0) if t is not None), adapters.shape[0] if adapters.shape else out)
+    if out is None or (adapters.shape is not None and adapters.shape != (out, inn)):
+        raise ValueError("x, y and the adapters disagree in shape")
+    if y is None:
+        y = torch.empty((T, out), dtype=torch.float16, device=x.device)
+    _lora_rows(y, T, out, "y")
+    _lora_rows(y0, T, out, "y0")
+    h_ld = _lora_h(h, T)
+    if workspace is None:
+        workspace = new_workspace(lora_workspace_bytes(T, 1, adapters.max_rank), x.device)
+    _here(x, y, y0, h, workspace, adapters.scale)
+    tok, keep = _tok_pointer(tenant_of_token, T)
+    _check(lib().bd_lora_multitenant(_ptr(x), adapters.a_ptrs, adapters.b_ptrs, adapters.rank_arr, _ptr(adapters.scale), tok, _ptr(y0),
+                                     _ptr(y), _ptr(h), h_ld, T, out, inn, adapters.n_tenants, _ptr(workspace), workspace.numel(),
+                                     _stream(stream)), "bd_lora_multitenant")
+    return y
+
+
+def lora_multitenant_group(x: torch.Tensor, group: LoraGroup, tenant_of_token, y0s: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                           ys: Optional[Sequence[torch.Tensor]] = None, hs: Optional[Sequence[torch.Tensor]] = None,
+                           workspace: Optional[torch.Tensor] = None, stream=None):
+    """bd_lora_multitenant_group: list of y_m fp16 [T, out_m].  hs: all or none, of one width."""
+    _dev(x, torch.float16, "x")
+    T, inn = x.shape
+    if group.inn is not None and group.inn != inn:
+        raise ValueError("x and the adapters disagree on `in`")
+    if ys is None:
+        ys = [torch.empty((T, o), dtype=torch.float16, device=x.device) for o in group.outs]
+    y0s = list(y0s) if y0s is not None else [None] * group.n
+    if len(ys) != group.n or len(y0s) != group.n or (hs is not None and len(hs) != group.n):
+        raise ValueError("one y (y0, h) per matrix")
+    for y, y0, o in zip(ys, y0s, group.outs):
+        _lora_rows(y, T, o, "y")
+        _lora_rows(y0, T, o, "y0")
+    widths = {_lora_h(h, T) for h in hs} if hs is not None else {0}
+    if len(widths) > 1:
+        raise ValueError("h of one width")
+    if workspace is None:
+        workspace = new_workspace(lora_workspace_bytes(T, group.n, group.max_rank), x.device)
+    _here(x, *ys, *y0s, *(hs or ()), workspace, *[t.scale for t in group.tables])
+    tok, keep = _tok_pointer(tenant_of_token, T)
+    ptrs = lambda ts: (ctypes.c_void_p * group.n)(*[_ptr(t) or None for t in ts])
+    _check(lib().bd_lora_multitenant_group(group.n, _ptr(x), group.a_ptrs, group.b_ptrs, group.rank_arr, group.scale, tok, ptrs(y0s),
+                                           ptrs(ys), ptrs(hs) if hs is not None else None, widths.pop(), T, group.out_arr, inn,
+                                           group.n_tenants, _ptr(workspace), workspace.numel(), _stream(stream)),
+           "bd_lora_multitenant_group")
+    return list(ys)
+
+
+class LoraGrads:
+    """Where the gradients of one matrix's adapters go: float32 device tensors of A's and B's shapes (or of as many elements),
+    None where a gradient is not wanted."""
+
+    def __init__(self, adapters: LoraTable, da_by_tenant: Sequence[Optional[torch.Tensor]], db_by_tenant: Sequence[Optional[torch.Tensor]]):
+        self.da, self.db, self.table = list(da_by_tenant), list(db_by_tenant), adapters
+        if len(self.da) != adapters.n_tenants or len(self.db) != adapters.n_tenants:
+            raise ValueError("one dA and one dB (or None) per tenant")
+        for grads, weights, what in ((self.da, adapters.a, "dA"), (self.db, adapters.b, "dB")):
+            for g, w in zip(grads, weights):
+                if g is not None:
+                    _dev(g, torch.float32, what)
+                    if w is None or g.numel() != w.numel():
+                        raise ValueError(f"{what} has the elements of its matrix")
+        n = max(adapters.n_tenants, 1)
+        self.da_ptrs = (ctypes.c_void_p * n)(*[_ptr(g) or None for g in self.da])
+        self.db_ptrs = (ctypes.c_void_p * n)(*[_ptr(g) or None for g in self.db])
+
+
+def lora_multitenant_backward(dy: torch.Tensor, x: Optional[torch.Tensor], h: Optional[torch.Tensor], adapters: LoraTable, tenant_of_token,
+                              grads: Optional[LoraGrads], dx0: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                              want_dx: bool = True, accumulate: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
+    """bd_lora_multitenant_backward: fills `grads` (accumulate: adds to them) and returns dx fp16 [T, in] = dx0 + what comes through the
+    adapters (None if want_dx is False).  x, h: what the forward call had and gave; x may be None where no dA, h where no dB is wanted."""
+    _dev(dy, torch.float16, "dy")
+    T, out = dy.shape
+    if adapters.shape is None:
+        raise ValueError("no tenant has an adapter")
+    inn = adapters.shape[1]
+    if adapters.shape[0] != out or (grads is not None and grads.table is not adapters):
+        raise ValueError("dy, the adapters and the gradients belong together")
+    if want_dx and dx is None:
+        dx = torch.empty((T, inn), dtype=torch.float16, device=dy.device)
+    if not want_dx:
+        dx = dx0 = None
+    for t, what in ((x, "x"), (dx0, "dx0"), (dx, "dx")):
+        _lora_rows(t, T, inn, what)
+    h_ld = _lora_h(h, T)
+    if workspace is None:
+        workspace = new_workspace(lora_backward_workspace_bytes(T, out, inn, adapters.max_rank), dy.device)
+    _here(dy, x, h, dx0, dx, workspace, adapters.scale)
+    tok, keep = _tok_pointer(tenant_of_token, T)
+    _check(lib().bd_lora_multitenant_backward(_ptr(dy), _ptr(x), _ptr(h), h_ld, adapters.a_ptrs, adapters.b_ptrs, adapters.rank_arr,
+                                              _ptr(adapters.scale), tok, _ptr(dx0), _ptr(dx), grads.da_ptrs if grads else None,
+                                              grads.db_ptrs if grads else None, int(accumulate), T, out, inn, adapters.n_tenants,
+                                              _ptr(workspace), workspace.numel(), _stream(stream)), "bd_lora_multitenant_backward")
+    return dx
+
+
+# ---- AdamW ---------------------------------------------------------------------------------------------
+
+ADAMW_BLOCK = 256
+
+
+class AdamWGroup:
+    """A plan (bd_adamw_plan) over fixed tensors: params float32, grads float32 or float16, states float32 or, with the two lists of
+    scales (float32, one per 256 elements), uint8; params_f16: the copies that the step writes, None where there is none."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], exp_avgs: Sequence[torch.Tensor],
+                 exp_avg_sqs: Sequence[torch.Tensor], params_f16: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                 exp_avg_scales: Optional[Sequence[torch.Tensor]] = None, exp_avg_sq_scales: Optional[Sequence[torch.Tensor]] = None):
+        n = len(params)
+        if (exp_avg_scales is None) != (exp_avg_sq_scales is None):
+            raise ValueError("scales for both states or for neither")
+        bits8 = exp_avg_scales is not None
+        lists = [list(params), list(grads), list(exp_avgs), list(exp_avg_sqs), list(params_f16) if params_f16 is not None else [None] * n,
+                 list(exp_avg_scales) if bits8 else [None] * n, list(exp_avg_sq_scales) if bits8 else [None] * n]
+        if any(len(l) != n for l in lists):
+            raise ValueError("one gradient, one of each state (copy, scale) per parameter")
+        grad_type = lists[1][0].dtype if n else torch.float32
+        if grad_type not in (torch.float32, torch.float16):
+            raise TypeError(f"gradients are float32 or float16, got {grad_type}")
+        state = torch.uint8 if bits8 else torch.float32
+        self.device = lists[0][0].device if n else None
+        for p, g, m, v, p16, ms, vs in zip(*lists):
+            for t, dtype, what in ((p, torch.float32, "param"), (g, grad_type, "grad"), (m, state, "exp_avg"), (v, state, "exp_avg_sq"),
+                                   (p16, torch.float16, "param_f16"), (ms, torch.float32, "scale"), (vs, torch.float32, "scale")):
+                if t is None:
+                    continue
+                _dev(t, dtype, what)
+                if t.device != self.device:
+                    raise ValueError("the tensors of a plan are on one device")
+                if t.numel() != (-(-p.numel() // ADAMW_BLOCK) if what == "scale" else p.numel()):
+                    raise ValueError(f"{what} does not fit its parameter")
+        self.keep, self.n = lists, n
+        ptrs = lambda ts: (ctypes.c_void_p * max(n, 1))(*[_ptr(t) or None for t in ts])
+        numel = (ctypes.c_int64 * max(n, 1))(*[int(p.numel()) for p in lists[0]])
+        self.bytes = int(lib().bd_adamw_plan_bytes(n))
+        self.plan = (ctypes.c_uint64 * max((self.bytes + 7) // 8, 1))()
+        _check(lib().bd_adamw_plan(self.plan, self.bytes, n, ptrs(lists[0]), ptrs(lists[4]), ptrs(lists[1]), int(grad_type == torch.float16),
+                                   ptrs(lists[2]), ptrs(lists[3]), ptrs(lists[5]) if bits8 else None, ptrs(lists[6]) if bits8 else None,
+                                   numel), "bd_adamw_plan")
+
+
+def adamw(group: AdamWGroup, lr: torch.Tensor, step: torch.Tensor, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+          weight_decay: float = 0.01, grad_scale: Optional[torch.Tensor] = None, skip: Optional[torch.Tensor] = None, stream=None) -> None:
+    """bd_adamw: one step of every tensor of the plan, in place.  lr float32 [1], step int64 [1] (1 for the first step), grad_scale
+    float32 [1] and skip int32 [1] are device tensors, read when the step runs."""
+    for t, dtype, what in ((lr, torch.float32, "lr"), (step, torch.int64, "step"), (grad_scale, torch.float32, "grad_scale"),
+                           (skip, torch.int32, "skip")):
+        if t is not None and _dev(t, dtype, what).numel() != 1:
+            raise ValueError(f"{what} is one number")
+    if group.n:
+        _here(lr, step, grad_scale, skip, group.keep[0][0])
+    _check(lib().bd_adamw(group.plan, group.bytes, _ptr(lr), _ptr(step), _ptr(grad_scale), _ptr(skip), beta1, beta2, eps, weight_decay,
+                          _stream(stream)), "bd_adamw")

@@ -7,6 +7,7 @@
 #include <utility>
 #include <vector>
 
+#include "bd_host.h"
 #include "bd_launch.h"
 #include "bd_tiled.h"
 
@@ -26,12 +27,9 @@ constexpr int kVariantPrefillMerged = 8;     // ... one product on W + alpha S, 
 constexpr int kVariantWide = 10;             // the kernel for tens to a few hundred tokens; 16 R + n: R row blocks and up to n column tiles per workgroup
 constexpr int kVariantPanels = 128;          // panels, row-major; + n: up to n column tiles per workgroup
 
-inline bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
-
-inline bool overlaps(const void* a, size_t abytes, const void* b, size_t bbytes) {
-    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
-    return a0 < b0 + bbytes && b0 < a0 + abytes;
-}
+using bd::misaligned;
+using bd::order_by_tenant;
+using bd::overlaps;
 
 // Tokens [t0, t0 + n) of the call -> one launch's bookkeeping: columns sorted by tenant
 // (stable), jobs = runs of equal tenant cut at the 16-column tile boundary.
@@ -124,23 +122,6 @@ size_t tiled_gemm_workspace_bytes(int64_t T, int32_t n_tenants) {
     return tables + (((size_t)n_tenants * 8 + 8 + 255) & ~(size_t)255);
 }
 
-// Token ids by tenant, tokens of one tenant in their order.  (Tenant ids have been checked.)
-std::vector<int32_t> order_by_tenant(const int32_t* tenant_of_token, int64_t T, int32_t n_tenants) {
-    std::vector<int32_t> order((size_t)T);
-    if (std::is_sorted(tenant_of_token, tenant_of_token + T)) {
-        for (int64_t i = 0; i < T; ++i) order[(size_t)i] = (int32_t)i;
-    } else if (n_tenants <= 8 * T) {
-        std::vector<int32_t> next((size_t)n_tenants + 1, 0);
-        for (int64_t i = 0; i < T; ++i) ++next[(size_t)tenant_of_token[i] + 1];
-        for (int32_t t = 0; t < n_tenants; ++t) next[(size_t)t + 1] += next[(size_t)t];
-        for (int64_t i = 0; i < T; ++i) order[(size_t)next[(size_t)tenant_of_token[i]]++] = (int32_t)i;
-    } else {   // a table of counts would be larger than the batch
-        for (int64_t i = 0; i < T; ++i) order[(size_t)i] = (int32_t)i;
-        std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return tenant_of_token[a] < tenant_of_token[b]; });
-    }
-    return order;
-}
-
 int cus_or_256() {
     int cus = 256;
     if (bd::device_cu_count(&cus) != hipSuccess || cus < 1) cus = 256;
@@ -204,34 +185,8 @@ hipError_t run_prefill(const uint16_t* x, const void* w, const uint32_t* const* 
         }
     }
     int32_t* dst = (int32_t*)workspace;
-    // The tables as runs of values that count up or repeat (tokens that arrive grouped by tenant: a few runs for the
-    // whole batch), where that takes fewer launches than the values themselves.
-    std::vector<int32_t> runs;   // triples: first index, first value, n (> 0 counting up, < 0 repeated)
-    for (size_t i = 0; i < all.size();) {
-        size_t e = i + 1;
-        const int32_t step = e < all.size() ? all[e] - all[i] : 0;
-        if (step == 0 || step == 1)
-            while (e < all.size() && all[e] - all[e - 1] == step) ++e;
-        runs.insert(runs.end(), {(int32_t)i, all[i], step == 1 ? (int32_t)(e - i) : -(int32_t)(e - i)});
-        i = e;
-    }
-    if ((runs.size() / 3 + 319) / 320 < (all.size() + 959) / 960) {
-        for (size_t off = 0; off < runs.size(); off += 960) {
-            bd::PrefillMetaChunk c;
-            const int n = (int)std::min<size_t>(960, runs.size() - off);
-            std::memcpy(c.v, runs.data() + off, (size_t)n * sizeof(int32_t));
-            const hipError_t e = bd::launch_prefill_meta_runs(c, dst, n / 3, st);
-            if (e != hipSuccess) return e;
-        }
-    } else {
-        for (size_t off = 0; off < all.size(); off += 960) {
-            bd::PrefillMetaChunk c;
-            const int n = (int)std::min<size_t>(960, all.size() - off);
-            std::memcpy(c.v, all.data() + off, (size_t)n * sizeof(int32_t));
-            const hipError_t e = bd::launch_prefill_meta(c, dst + off, n, st);
-            if (e != hipSuccess) return e;
-        }
-    }
+    const hipError_t written = bd::write_int_table(all, dst, st);
+    if (written != hipSuccess) return written;
     if (tiled) packed_by_tenant = (const uint32_t* const*)(dst + pointer_table_at);
     if (merged)
         return bd::launch_linear_prefill_merged(x, (const uint16_t*)w, packed_by_tenant, alpha_by_tenant, dst,

@@ -1,0 +1,475 @@
+// C ABI of the low-rank adapters (include/bitdelta.h): argument checks, token grouping, launches.  Everything here runs on the
+// host; nothing is enqueued before the arguments have passed.
+#include "bitdelta.h"
+
+#include <cstring>
+#include <memory>
+#include <vector>
+
+#include "bd_host.h"
+#include "bd_lora.h"
+
+namespace {
+
+using bd::misaligned;
+using bd::overlaps;
+
+constexpr int kFewColumns = 16, kManyColumns = 64;   // tokens of a tile: records are tiles, or jobs
+constexpr int64_t kFewTokens = 512;                  // largest batch whose records are tiles
+constexpr int kGradParts = 16;                       // jobs x parts of the tokens of a gradient, where there is more than one part
+
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// Parts that the shrink's sum may be cut into: few tokens leave compute units idle.
+int max_splits(int64_t T) { return T <= 2048 ? 8 : T <= 8192 ? 4 : T <= 16384 ? 2 : 1; }
+int sum_splits(int64_t groups, int64_t K, int64_t T) {
+    const int64_t steps = (K + 31) / 32;   // 8 wavefronts with at least 4 steps each
+    const int64_t most = std::min<int64_t>(max_splits(T), steps / (4 * bd::kLoraShrinkWaves)), want = (256 + groups - 1) / groups;
+    return (int)std::max<int64_t>(1, std::min(most, want));
+}
+
+struct Job {
+    int32_t tenant, first, count;   // first: position in the sorted order
+};
+
+// The batch by tenant.
+struct Batch {
+    std::vector<int32_t> order;   // empty: the tokens are sorted as they come
+    std::vector<Job> jobs;
+    int32_t token(int64_t p) const { return order.empty() ? (int32_t)p : order[(size_t)p]; }
+};
+Batch group(const int32_t* tenant_of_token, int64_t T, int32_t n_tenants) {
+    Batch b;
+    if (!std::is_sorted(tenant_of_token, tenant_of_token + T)) b.order = bd::order_by_tenant(tenant_of_token, T, n_tenants);
+    for (int64_t p = 0; p < T; ++p) {
+        const int32_t tenant = tenant_of_token[b.token(p)];
+        if (b.jobs.empty() || b.jobs.back().tenant != tenant) b.jobs.push_back(Job{tenant, (int32_t)p, 0});
+        ++b.jobs.back().count;
+    }
+    return b;
+}
+
+// Fills the records of one kernel's launches and runs them: `per_record` says whether a (job, matrix) takes part, with which
+// weight and rank.
+template <typename Args, typename Weight, typename Launch>
+hipError_t for_records(Args& a, const Batch& b, int64_t T, int n_mats, bool few, Weight weight, Launch launch) {
+    int n = 0, tiles = 0, max_rank = 0;
+    auto flush = [&]() -> hipError_t {
+        if (n == 0) return hipSuccess;
+        a.n_records = n;
+        a.n_tiles = tiles;
+        const hipError_t e = launch(max_rank);
+        n = tiles = max_rank = 0;
+        return e;
+    };
+    for (const Job& j : b.jobs)
+        for (int m = 0; m < n_mats; ++m) {
+            const uint16_t* w = nullptr;
+            int rank = 0;
+            if (!weight(m, j.tenant, &w, &rank)) continue;
+            if (few) {
+                for (int32_t at = 0; at < j.count; at += kFewColumns) {
+                    bd::LoraTile& t = a.tile[n];
+                    t = bd::LoraTile{};
+                    t.w = w;
+                    t.hrow = (int32_t)(m * T + j.first + at);
+                    t.tenant = j.tenant;
+                    t.rank = (uint16_t)rank;
+                    t.count = (uint16_t)std::min(kFewColumns, j.count - at);
+                    t.mat = (uint16_t)m;
+                    for (int c = 0; c < t.count; ++c) t.col[c] = (uint16_t)b.token(j.first + at + c);
+                    ++n, ++tiles;
+                    max_rank = std::max(max_rank, rank);
+                    if (n == bd::kLoraRecords)
+                        if (const hipError_t e = flush(); e != hipSuccess) return e;
+                }
+            } else {
+                bd::LoraJob& t = a.job[n];
+                t = bd::LoraJob{};
+                t.w = w;
+                t.hrow = (int32_t)(m * T + j.first);
+                t.tenant = j.tenant;
+                t.count = j.count;
+                t.tile_begin = tiles;
+                t.first = j.first;
+                t.rank = (uint16_t)rank;
+                t.mat = (uint16_t)m;
+                ++n;
+                tiles += (j.count + kManyColumns - 1) / kManyColumns;
+                max_rank = std::max(max_rank, rank);
+                if (n == bd::kLoraRecords)
+                    if (const hipError_t e = flush(); e != hipSuccess) return e;
+            }
+        }
+    return flush();
+}
+
+// The workspace: the order of the tokens, then h (or g) as partial sums.
+struct Workspace {
+    int32_t* order;
+    float* h;
+    float* partial;
+};
+size_t order_bytes(int64_t T) { return (size_t)round_up(T * 4, 256); }
+size_t h_bytes(int64_t T, int32_t n_mats, int32_t max_rank) {
+    return (size_t)round_up((int64_t)max_splits(T) * n_mats * T * round_up(max_rank, 16) * 4, 256);
+}
+size_t grad_part_bytes(int64_t out, int64_t in, int32_t max_rank) {
+    return (size_t)round_up((int64_t)kGradParts * round_up(max_rank, 16) * (in + out) * 4, 256);
+}
+
+bool sizes_ok(int64_t T, int64_t out, int64_t in, int32_t n_tenants) {
+    return T >= 0 && T <= 65535 && out >= 0 && in >= 0 && n_tenants >= 0 && in % 32 == 0 && out <= (int64_t)1 << 24 && in <= (int64_t)1 << 24;
+}
+
+bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by, const uint16_t* const* b_by, const int32_t* rank_by,
+                  const float* const* scale, const int32_t* tenant_of_token, const uint16_t* const* y0, uint16_t* const* y,
+                  float* const* h, int32_t h_ld, int64_t T, const int64_t* out, int64_t in, int32_t n_tenants, void* workspace,
+                  size_t workspace_bytes, hipStream_t st) {
+    if (n_mats < 1 || n_mats > bd::kLoraMaxMats) return BD_ERR_SHAPE;
+    if (!out) return BD_ERR_NULL;
+    for (int m = 0; m < n_mats; ++m)
+        if (!sizes_ok(T, out[m], in, n_tenants)) return BD_ERR_SHAPE;
+    if (T == 0) return BD_OK;
+    if (!a_by || !b_by || !rank_by || !scale || !tenant_of_token || !y) return BD_ERR_NULL;
+    for (int64_t t = 0; t < T; ++t)
+        if (tenant_of_token[t] < 0 || tenant_of_token[t] >= n_tenants) return BD_ERR_TENANT;
+    const Batch batch = group(tenant_of_token, T, n_tenants);
+    int max_rank = 0;
+    int64_t max_out = 0;
+    for (int m = 0; m < n_mats; ++m) max_out = std::max(max_out, out[m]);
+    for (const Job& j : batch.jobs)
+        for (int m = 0; m < n_mats; ++m) {
+            const int32_t rank = rank_by[(size_t)m * n_tenants + j.tenant];
+            if (rank < 0 || rank > bd::kLoraMaxRank) return BD_ERR_SHAPE;
+            max_rank = std::max(max_rank, (int)rank);
+        }
+    if (max_rank > 0 && in > 0 && !x) return BD_ERR_NULL;
+    if (misaligned(x, 16)) return BD_ERR_ALIGN;
+    const size_t xbytes = (size_t)T * in * 2;
+    for (int m = 0; m < n_mats; ++m) {
+        const size_t ybytes = (size_t)T * out[m] * 2;
+        if (out[m] > 0 && !y[m]) return BD_ERR_NULL;
+        if (misaligned(y[m], 16) || (y0 && misaligned(y0[m], 16)) || misaligned(scale[m], 4) || (h && misaligned(h[m], 4))) return BD_ERR_ALIGN;
+        if (max_rank > 0 && out[m] > 0 && !scale[m]) return BD_ERR_NULL;
+        const size_t hbytes = h && h[m] ? (size_t)T * h_ld * 4 : 0;
+        if (hbytes && h_ld < max_rank) return BD_ERR_SHAPE;
+        if (overlaps(y[m], ybytes, x, xbytes) || (hbytes && (overlaps(h[m], hbytes, x, xbytes) || overlaps(h[m], hbytes, y[m], ybytes)))) return BD_ERR_ALIAS;
+        for (int o = 0; o < n_mats; ++o) {
+            const size_t obytes = (size_t)T * out[o] * 2;
+            if (o != m && overlaps(y[m], ybytes, y[o], obytes)) return BD_ERR_ALIAS;
+            if (o != m && hbytes && (overlaps(h[m], hbytes, y[o], obytes) || (h[o] && overlaps(h[m], hbytes, h[o], (size_t)T * h_ld * 4)))) return BD_ERR_ALIAS;
+            if (y0 && y0[o] && !(o == m && y0[m] == y[m]) && overlaps(y[m], ybytes, y0[o], obytes)) return BD_ERR_ALIAS;
+            if (y0 && y0[o] && hbytes && overlaps(h[m], hbytes, y0[o], obytes)) return BD_ERR_ALIAS;
+        }
+    }
+    for (const Job& j : batch.jobs)
+        for (int m = 0; m < n_mats; ++m) {
+            const size_t at = (size_t)m * n_tenants + j.tenant;
+            const size_t rank = (size_t)rank_by[at], abytes = rank * in * 2, bbytes = rank * out[m] * 2;
+            if (rank == 0) continue;
+            if ((abytes && !a_by[at]) || (bbytes && !b_by[at])) return BD_ERR_NULL;
+            if (misaligned(a_by[at], 16) || misaligned(b_by[at], 16)) return BD_ERR_ALIGN;
+            for (int o = 0; o < n_mats; ++o) {
+                const size_t ybytes = (size_t)T * out[o] * 2, hbytes = h && h[o] ? (size_t)T * h_ld * 4 : 0;
+                if (overlaps(y[o], ybytes, a_by[at], abytes) || overlaps(y[o], ybytes, b_by[at], bbytes)) return BD_ERR_ALIAS;
+                if (hbytes && (overlaps(h[o], hbytes, a_by[at], abytes) || overlaps(h[o], hbytes, b_by[at], bbytes))) return BD_ERR_ALIAS;
+            }
+        }
+    if (max_rank > 0 && (!workspace || workspace_bytes < order_bytes(T) + h_bytes(T, n_mats, max_rank) || misaligned(workspace, 256)))
+        return BD_ERR_WORKSPACE;
+    // ---- checked: launches from here on ----
+    const bool few = T <= kFewTokens;
+    const int columns = few ? kFewColumns : kManyColumns;
+    const int32_t* order = nullptr;
+    if (!few && !batch.order.empty() && max_rank > 0) {
+        if (bd::write_int_table(batch.order, (int32_t*)workspace, st) != hipSuccess) return BD_ERR_DEVICE;
+        order = (const int32_t*)workspace;
+    }
+    float* const hw = (float*)((char*)workspace + order_bytes(T));
+    const int64_t ld = round_up(max_rank, 16);
+    int64_t tiles = 0;
+    for (const Job& j : batch.jobs)
+        for (int m = 0; m < n_mats; ++m)
+            tiles += (int64_t)(j.count + columns - 1) / columns * ((rank_by[(size_t)m * n_tenants + j.tenant] + 15) / 16);
+    const int splits = sum_splits(std::max<int64_t>(tiles, 1), in, T);
+    if (max_rank > 0) {
+        auto s = std::make_unique<bd::LoraShrinkArgs>();
+        s->src = x;
+        s->order = order;
+        s->h = hw;
+        s->K = in;
+        s->ld = (int32_t)ld;
+        s->splits = splits;
+        s->split_stride = n_mats * T * ld;
+        const hipError_t e = for_records(
+            *s, batch, T, n_mats, few,
+            [&](int m, int32_t tenant, const uint16_t** w, int* rank) {
+                const size_t at = (size_t)m * n_tenants + tenant;
+                *w = a_by[at];
+                *rank = rank_by[at];
+                return rank_by[at] > 0;
+            },
+            [&](int rank) { return bd::launch_lora_shrink(*s, columns, false, rank, st); });
+        if (e != hipSuccess) return BD_ERR_DEVICE;
+    }
+    auto x2 = std::make_unique<bd::LoraExpandArgs>();
+    for (int m = 0; m < n_mats; ++m) {
+        x2->y0[m] = y0 ? y0[m] : nullptr;
+        x2->y[m] = y[m];
+        x2->scale[m] = scale[m];
+        x2->F[m] = out[m];
+        x2->h_out[m] = h ? h[m] : nullptr;
+    }
+    x2->h = hw;
+    x2->order = order;
+    x2->ld = (int32_t)ld;
+    x2->h_ld = h_ld;
+    x2->splits = splits;
+    x2->split_stride = n_mats * T * ld;
+    const hipError_t e = for_records(
+        *x2, batch, T, n_mats, few,
+        [&](int m, int32_t tenant, const uint16_t** w, int* rank) {
+            const size_t at = (size_t)m * n_tenants + tenant;
+            *w = b_by[at];
+            *rank = rank_by[at];
+            // without an adapter there is nothing to do where y is y0
+            return (out[m] > 0 || (h && h[m])) && (rank_by[at] > 0 || !(y0 && y0[m] == y[m]));
+        },
+        [&](int) { return bd::launch_lora_expand(*x2, columns, false, max_out, st); });
+    return e == hipSuccess ? BD_OK : BD_ERR_DEVICE;
+}
+
+bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_t h_ld, const uint16_t* const* a_by, const uint16_t* const* b_by,
+                   const int32_t* rank_by, const float* scale, const int32_t* tenant_of_token, const uint16_t* dx0, uint16_t* dx,
+                   float* const* da_by, float* const* db_by, int32_t accumulate, int64_t T, int64_t out, int64_t in, int32_t n_tenants,
+                   void* workspace, size_t workspace_bytes, hipStream_t st) {
+    if (!sizes_ok(T, out, in, n_tenants)) return BD_ERR_SHAPE;
+    if (n_tenants > 0 && !rank_by) return BD_ERR_NULL;
+    if (T > 0 && !tenant_of_token) return BD_ERR_NULL;
+    for (int64_t t = 0; t < T; ++t)
+        if (tenant_of_token[t] < 0 || tenant_of_token[t] >= n_tenants) return BD_ERR_TENANT;
+    const Batch batch = group(tenant_of_token, T, n_tenants);
+    std::vector<bd::Range> ranges;
+    auto range = [&](const void* p, size_t bytes, bool written) { bd::add_range(ranges, p, bytes, written); };
+    int max_rank = 0;
+    bool any_da = false, any_db = false;
+    std::vector<char> has_tokens((size_t)n_tenants, 0);
+    for (const Job& j : batch.jobs) {
+        const int32_t e = j.tenant, rank = rank_by[e];
+        has_tokens[(size_t)e] = 1;
+        if (rank < 0 || rank > bd::kLoraMaxRank) return BD_ERR_SHAPE;
+        max_rank = std::max(max_rank, (int)rank);
+        if (rank == 0) continue;
+        const size_t abytes = (size_t)rank * in * 2, bbytes = (size_t)rank * out * 2;
+        const bool da = da_by && da_by[e], db = db_by && db_by[e];
+        any_da |= da;
+        any_db |= db;
+        if (dx && abytes && (!a_by || !a_by[e])) return BD_ERR_NULL;
+        if ((dx || da) && bbytes && (!b_by || !b_by[e])) return BD_ERR_NULL;
+        if ((a_by && misaligned(a_by[e], 16)) || (b_by && misaligned(b_by[e], 16))) return BD_ERR_ALIGN;
+        if (dx && a_by) range(a_by[e], abytes, false);
+        if ((dx || da) && b_by) range(b_by[e], bbytes, false);
+    }
+    for (int32_t e = 0; e < n_tenants; ++e) {
+        const bool da = da_by && da_by[e], db = db_by && db_by[e];
+        if (!da && !db) continue;
+        if (rank_by[e] < 0 || rank_by[e] > bd::kLoraMaxRank) return BD_ERR_SHAPE;
+        if ((da && misaligned(da_by[e], 16)) || (db && misaligned(db_by[e], 16))) return BD_ERR_ALIGN;
+        if (!has_tokens[(size_t)e] && accumulate) continue;
+        if (da) range(da_by[e], (size_t)rank_by[e] * in * 4, true);
+        if (db) range(db_by[e], (size_t)rank_by[e] * out * 4, true);
+    }
+    const bool work = T > 0 && max_rank > 0, want_dx = dx && T > 0 && in > 0;
+    if (work) {
+        if (out > 0 && (dx || any_da || any_db) && !dy) return BD_ERR_NULL;
+        if (in > 0 && any_da && !x) return BD_ERR_NULL;
+        if (out > 0 && any_db && !h) return BD_ERR_NULL;
+        if ((dx || any_da || any_db) && !scale) return BD_ERR_NULL;
+        if (any_db && h_ld < max_rank) return BD_ERR_SHAPE;
+    }
+    if (misaligned(dy, 16) || misaligned(x, 16) || misaligned(h, 4) || misaligned(scale, 4) || misaligned(dx0, 16) || misaligned(dx, 16)) return BD_ERR_ALIGN;
+    range(dy, (size_t)T * out * 2, false);
+    range(x, (size_t)T * in * 2, false);
+    if (any_db) range(h, (size_t)T * h_ld * 4, false);
+    if (want_dx) {
+        range(dx, (size_t)T * in * 2, true);
+        if (dx0 != dx) range(dx0, (size_t)T * in * 2, false);
+    }
+    if (bd::any_alias(ranges)) return BD_ERR_ALIAS;
+    if (work && (!workspace || misaligned(workspace, 256) || workspace_bytes < bd_lora_backward_workspace_bytes(T, out, in, max_rank)))
+        return BD_ERR_WORKSPACE;
+    // ---- checked: launches from here on ----
+    const bool few = T <= kFewTokens;
+    const int columns = few ? kFewColumns : kManyColumns;
+    const int64_t ld = round_up(max_rank, 16);
+    const int32_t* order = nullptr;
+    if (work && !batch.order.empty()) {   // (the gradients' sums run over a job's tokens, for few tokens too)
+        if (bd::write_int_table(batch.order, (int32_t*)workspace, st) != hipSuccess) return BD_ERR_DEVICE;
+        order = (const int32_t*)workspace;
+    }
+    float* const g = work ? (float*)((char*)workspace + order_bytes(T)) : nullptr;
+    float* const partial = work ? (float*)((char*)g + h_bytes(T, 1, max_rank)) : nullptr;
+    int64_t tiles = 0;
+    for (const Job& j : batch.jobs) tiles += (int64_t)(j.count + columns - 1) / columns * ((rank_by[j.tenant] + 15) / 16);
+    const int splits = sum_splits(std::max<int64_t>(tiles, 1), out, T);
+    auto weights_of = [&](const uint16_t* const* by, bool all) {
+        return [=](int, int32_t tenant, const uint16_t** w, int* rank) {
+            *rank = rank_by[tenant];
+            *w = by && *rank > 0 ? by[tenant] : nullptr;
+            return all || *rank > 0;
+        };
+    };
+    if (work && (want_dx || any_da)) {
+        auto s = std::make_unique<bd::LoraShrinkArgs>();
+        s->src = dy;
+        s->scale = scale;
+        s->order = order;
+        s->h = g;
+        s->K = out;
+        s->ld = (int32_t)ld;
+        s->splits = splits;
+        s->split_stride = T * ld;
+        if (for_records(*s, batch, T, 1, few, weights_of(b_by, false), [&](int rank) { return bd::launch_lora_shrink(*s, columns, true, rank, st); }) != hipSuccess)
+            return BD_ERR_DEVICE;
+    }
+    if (want_dx) {
+        auto x2 = std::make_unique<bd::LoraExpandArgs>();
+        x2->y0[0] = dx0;
+        x2->y[0] = dx;
+        x2->F[0] = in;
+        x2->h = g;
+        x2->order = order;
+        x2->ld = (int32_t)ld;
+        x2->splits = splits;
+        x2->split_stride = T * ld;
+        if (for_records(*x2, batch, T, 1, few, weights_of(a_by, dx0 != dx), [&](int) { return bd::launch_lora_expand(*x2, columns, true, in, st); }) != hipSuccess)
+            return BD_ERR_DEVICE;
+    }
+    for (int which = 0; which < 2 && work; ++which) {   // dA, then dB
+        float* const* const by = which ? db_by : da_by;
+        const int64_t F = which ? out : in;
+        if (!(which ? any_db : any_da) || F == 0) continue;
+        auto args = std::make_unique<bd::LoraGradArgs>();
+        auto sum = std::make_unique<bd::LoraReduceArgs>();
+        args->d = which ? dy : x;
+        args->w = which ? h : g;
+        args->scale = which ? scale : nullptr;
+        args->order = order;
+        args->F = F;
+        args->w_ld = which ? h_ld : (int32_t)ld;
+        args->w_splits = which ? 1 : splits;
+        args->w_split_stride = T * ld;
+        args->accumulate = sum->accumulate = accumulate ? 1 : 0;
+        args->w_by_token = which;
+        args->rank_major = !which;
+        args->partial = partial + (which ? (int64_t)kGradParts * ld * in : 0);
+        sum->partial = args->partial;
+        std::vector<Job> wanted;
+        for (const Job& j : batch.jobs)
+            if (rank_by[j.tenant] > 0 && by[j.tenant]) wanted.push_back(j);
+        for (size_t first = 0; first < wanted.size(); first += bd::kLoraRecords) {
+            const int n = (int)std::min<size_t>(bd::kLoraRecords, wanted.size() - first);
+            int64_t part = 0, max_n = 0;
+            int most = 0, longest = 0;
+            for (int i = 0; i < n; ++i) {
+                const Job& j = wanted[first + (size_t)i];
+                const int rank = rank_by[j.tenant];
+                args->job[i] = bd::LoraGradJob{by[j.tenant], part, j.tenant, j.count, j.first, rank};
+                sum->job[i].out = by[j.tenant];
+                sum->job[i].part = part;
+                sum->job[i].n = rank * F;
+                part += rank * F;
+                max_n = std::max(max_n, rank * F);
+                most = std::max(most, rank);
+                longest = std::max(longest, (int)j.count);
+            }
+            const int64_t groups = n * ((F + bd::kLoraFeatures - 1) / bd::kLoraFeatures);
+            args->n_jobs = sum->n_jobs = n;
+            // few workgroups: the tokens of a job in parts of at least 256
+            args->token_splits = sum->token_splits =
+                (int)std::max<int64_t>(1, std::min({(512 + groups - 1) / groups, (int64_t)kGradParts / n, (int64_t)longest / 256}));
+            args->part_stride = sum->part_stride = part;
+            if (bd::launch_lora_grad(*args, most, st) != hipSuccess) return BD_ERR_DEVICE;
+            if (args->token_splits > 1 && bd::launch_lora_reduce(*sum, max_n, st) != hipSuccess) return BD_ERR_DEVICE;
+        }
+    }
+    if (!accumulate) {   // gradients of adapters that no token used
+        auto zero = std::make_unique<bd::LoraReduceArgs>();
+        int n = 0;
+        int64_t max_n = 0;
+        auto flush = [&]() {
+            zero->n_jobs = n;
+            const bool ok = n == 0 || bd::launch_lora_reduce(*zero, max_n, st) == hipSuccess;
+            n = 0;
+            max_n = 0;
+            return ok;
+        };
+        for (int32_t e = 0; e < n_tenants; ++e) {
+            if (has_tokens[(size_t)e]) continue;
+            for (int which = 0; which < 2; ++which) {
+                float* const p = which ? (db_by ? db_by[e] : nullptr) : (da_by ? da_by[e] : nullptr);
+                const int64_t count = rank_by[e] * (which ? out : in);
+                if (!p || count == 0) continue;
+                zero->job[n].out = p;
+                zero->job[n].n = count;
+                max_n = std::max(max_n, count);
+                if (++n == bd::kLoraRecords && !flush()) return BD_ERR_DEVICE;
+            }
+        }
+        if (!flush()) return BD_ERR_DEVICE;
+    }
+    return BD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t bd_lora_workspace_bytes(int64_t T, int32_t n_mats, int32_t max_rank) {
+    if (T < 1 || T > 65535 || n_mats < 1 || n_mats > bd::kLoraMaxMats || max_rank < 1 || max_rank > bd::kLoraMaxRank) return 0;
+    return order_bytes(T) + h_bytes(T, n_mats, max_rank);
+}
+
+size_t bd_lora_backward_workspace_bytes(int64_t T, int64_t out, int64_t in, int32_t max_rank) {
+    if (T < 1 || !sizes_ok(T, out, in, 0) || max_rank < 1 || max_rank > bd::kLoraMaxRank) return 0;
+    return order_bytes(T) + h_bytes(T, 1, max_rank) + grad_part_bytes(out, in, max_rank);
+}
+
+// (what the standard library throws here is a lack of host memory)
+bd_status bd_lora_multitenant_group(int32_t n_mats, const uint16_t* x_f16, const uint16_t* const* a_by_mat_tenant,
+                                    const uint16_t* const* b_by_mat_tenant, const int32_t* rank_by_mat_tenant,
+                                    const float* const* scale_by_mat, const int32_t* tenant_of_token, const uint16_t* const* y0_f16,
+                                    uint16_t* const* y_f16, float* const* h, int32_t h_ld, int64_t T, const int64_t* out, int64_t in,
+                                    int32_t n_tenants, void* workspace, size_t workspace_bytes, void* stream) {
+    try {
+        return forward(n_mats, x_f16, a_by_mat_tenant, b_by_mat_tenant, rank_by_mat_tenant, scale_by_mat, tenant_of_token, y0_f16, y_f16, h,
+                       h_ld, T, out, in, n_tenants, workspace, workspace_bytes, (hipStream_t)stream);
+    } catch (...) {
+        return BD_ERR_DEVICE;
+    }
+}
+
+bd_status bd_lora_multitenant(const uint16_t* x_f16, const uint16_t* const* a_by_tenant, const uint16_t* const* b_by_tenant,
+                              const int32_t* rank_by_tenant, const float* scale_by_tenant, const int32_t* tenant_of_token,
+                              const uint16_t* y0_f16, uint16_t* y_f16, float* h, int32_t h_ld, int64_t T, int64_t out, int64_t in,
+                              int32_t n_tenants, void* workspace, size_t workspace_bytes, void* stream) {
+    return bd_lora_multitenant_group(1, x_f16, a_by_tenant, b_by_tenant, rank_by_tenant, &scale_by_tenant, tenant_of_token, &y0_f16, &y_f16,
+                                     &h, h_ld, T, &out, in, n_tenants, workspace, workspace_bytes, stream);
+}
+
+bd_status bd_lora_multitenant_backward(const uint16_t* dy_f16, const uint16_t* x_f16, const float* h, int32_t h_ld,
+                                       const uint16_t* const* a_by_tenant, const uint16_t* const* b_by_tenant,
+                                       const int32_t* rank_by_tenant, const float* scale_by_tenant, const int32_t* tenant_of_token,
+                                       const uint16_t* dx0_f16, uint16_t* dx_f16, float* const* da_by_tenant, float* const* db_by_tenant,
+                                       int32_t accumulate, int64_t T, int64_t out, int64_t in, int32_t n_tenants, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+    try {
+        return backward(dy_f16, x_f16, h, h_ld, a_by_tenant, b_by_tenant, rank_by_tenant, scale_by_tenant, tenant_of_token, dx0_f16, dx_f16,
+                        da_by_tenant, db_by_tenant, accumulate, T, out, in, n_tenants, workspace, workspace_bytes, (hipStream_t)stream);
+    } catch (...) {
+        return BD_ERR_DEVICE;
+    }
+}
+
+}  // extern "C"
