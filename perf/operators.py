@@ -355,7 +355,7 @@ def _own_grad(s):
         db = iter(torch.split(s["db"], [r * s["out"] for r in s["ranks"] if r]))
         s["grads"] = bd.LoraGrads(s["table"], [next(da) if r else None for r in s["ranks"]], [next(db) if r else None for r in s["ranks"]])
         s["dx"] = torch.empty_like(s["dx0"])
-        s["ws"] = bd.new_workspace(bd.lora_backward_workspace_bytes(T, s["out"], inn, max(s["ranks"])), DEVICE)
+        s["ws"] = bd.new_workspace(bd.lora_backward_workspace_bytes(T, s["out"], inn, len(s["ranks"]), max(s["ranks"])), DEVICE)
     dx = bd.lora_multitenant_backward(s["dy"], s["x"], s["h"], s["table"], s["tok"], s["grads"], dx0=s["dx0"], dx=s["dx"],
                                       workspace=s["ws"])
     return {"dx": dx, "da": s["da"], "db": s["db"]}
