@@ -473,13 +473,13 @@ bd_status bd_lora_multitenant_group(int32_t n_mats, const uint16_t* x_f16, const
  *     dB_e  = s_e * sum of dy[t] h[t]^T             binary32 [out, r_e]
  *   dy_f16 [T, out]; x_f16 and h as of the forward call (h_ld too); the other arguments as there
  *   dx_f16           [T, in], or NULL where it is not wanted
- *   da_by_tenant, db_by_tenant   HOST arrays of n_tenants DEVICE pointers (16-byte aligned), NULL where a gradient is not wanted;
+ *   da_by_tenant, db_by_tenant   HOST arrays of n_tenants DEVICE pointers (4-byte aligned), NULL where a gradient is not wanted;
  *                    either array may be NULL.  Inputs that no wanted result needs may be NULL.
  *   accumulate       0: the gradients are overwritten, those of tenants without a token with zeros; else they are added to
- *   workspace        bd_lora_backward_workspace_bytes(T, out, in, largest rank) bytes, 256-byte aligned, device memory
+ *   workspace        bd_lora_backward_workspace_bytes(T, out, in, n_tenants, largest rank) bytes, 256-byte aligned, device memory
  * Sums in binary32 in a fixed order: the same inputs give the same bits.  The ranks of tenants whose gradients are asked for are
  * checked too.  Two tenants may share A and B, but not their gradients (BD_ERR_ALIAS). */
-size_t bd_lora_backward_workspace_bytes(int64_t T, int64_t out, int64_t in, int32_t max_rank);
+size_t bd_lora_backward_workspace_bytes(int64_t T, int64_t out, int64_t in, int32_t n_tenants, int32_t max_rank);
 bd_status bd_lora_multitenant_backward(const uint16_t* dy_f16, const uint16_t* x_f16, const float* h, int32_t h_ld,
                                        const uint16_t* const* a_by_tenant, const uint16_t* const* b_by_tenant,
                                        const int32_t* rank_by_tenant, const float* scale_by_tenant, const int32_t* tenant_of_token,

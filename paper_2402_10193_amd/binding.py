@@ -122,7 +122,7 @@ def lib() -> ctypes.CDLL:
         L.bd_lora_multitenant.argtypes = [vp, pvp, pvp, pi, vp, vp, vp, vp, vp, i32, i64, i64, i64, i32, vp, sz, vp]
         L.bd_lora_multitenant_group.argtypes = [i32, vp, pvp, pvp, pi, pvp, vp, pvp, pvp, pvp, i32, i64, pi64, i64, i32, vp, sz, vp]
         L.bd_lora_backward_workspace_bytes.restype = sz
-        L.bd_lora_backward_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.bd_lora_backward_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
         L.bd_lora_multitenant_backward.argtypes = [vp, vp, vp, i32, pvp, pvp, pi, vp, vp, vp, vp, pvp, pvp, i32, i64, i64, i64, i32, vp, sz, vp]
         L.bd_adamw_plan_bytes.restype = sz
         L.bd_adamw_plan_bytes.argtypes = [i32]
@@ -903,8 +903,8 @@ def lora_workspace_bytes(T: int, n_mats: int, max_rank: int) -> int:
     return int(lib().bd_lora_workspace_bytes(T, n_mats, max_rank))
 
 
-def lora_backward_workspace_bytes(T: int, out: int, inn: int, max_rank: int) -> int:
-    return int(lib().bd_lora_backward_workspace_bytes(T, out, inn, max_rank))
+def lora_backward_workspace_bytes(T: int, out: int, inn: int, n_tenants: int, max_rank: int) -> int:
+    return int(lib().bd_lora_backward_workspace_bytes(T, out, inn, n_tenants, max_rank))
 
 
 class LoraTable:
@@ -1082,7 +1082,7 @@ def lora_multitenant_backward(dy: torch.Tensor, x: Optional[torch.Tensor], h: Op
         _lora_rows(t, T, inn, what)
     h_ld = _lora_h(h, T)
     if workspace is None:
-        workspace = new_workspace(lora_backward_workspace_bytes(T, out, inn, adapters.max_rank), dy.device)
+        workspace = new_workspace(lora_backward_workspace_bytes(T, out, inn, adapters.n_tenants, adapters.max_rank), dy.device)
     _here(dy, x, h, dx0, dx, workspace, adapters.scale)
     tok, keep = _tok_pointer(tenant_of_token, T)
     _check(lib().bd_lora_multitenant_backward(_ptr(dy), _ptr(x), _ptr(h), h_ld, adapters.a_ptrs, adapters.b_ptrs, adapters.rank_arr,

@@ -18,7 +18,7 @@ constexpr int kLoraRecords = 64;        // records of one launch
 constexpr int kLoraFeatures = 128;      // output features of one wavefront's step: 8 MFMA rows of 16
 constexpr int kLoraShrinkWaves = 8;
 constexpr int kLoraExpandWaves = 4;
-constexpr int kLoraGradWaves = 8;
+constexpr int kLoraGradWaves = 4;
 
 struct LoraTile {                       // few tokens
     const uint16_t* w;                  // the launch's weight: A or B of this tenant and matrix
@@ -66,34 +66,55 @@ struct LoraExpandArgs {
     };
 };
 
-// out[r][f] (dA) or out[f][r] (dB) = scale * sum over a job's tokens of w[token][r] d[token][f]
-struct LoraGradJob {
-    float* out;
-    int64_t part;                       // where the job's partial sums begin in `partial` (floats)
-    int32_t tenant, count, first;       // first: sorted position, also the row of w in position order
-    int32_t rank;
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+
+// g and h as operands of the gradients' sums over tokens, in chunks of 32 tokens of a job
+struct LoraPrepJob {
+    int32_t first, count, rank, chunk_begin;
 };
-struct LoraGradArgs {
-    const uint16_t* d;                  // [T, F]
-    const float* w;                     // dA: g [splits][rows][w_ld] by sorted position; dB: h [T, w_ld] by token
-    const float* scale;                 // dB: device, by tenant; dA: nullptr (g has it)
+struct LoraPrepArgs {
+    float* g;                           // [splits][rows][ld] by sorted position; part 0 receives the sum
+    const float* h;                     // [T, h_ld] by token
     const int32_t* order;
-    float* partial;                     // [token_splits][part_stride], used where token_splits > 1
-    int64_t F, w_split_stride, part_stride;
-    int32_t w_ld, w_splits, token_splits, n_jobs, accumulate, w_by_token, rank_major;   // rank_major: out is [rank][F]
-    LoraGradJob job[kLoraRecords];
-};
-// out (+)= sum over the splits of the partial sums; or zeros for gradients of tenants without a token
-struct LoraReduceArgs {
-    const float* partial;               // nullptr: zeros
-    int64_t part_stride;
-    int32_t token_splits, n_jobs, accumulate;
-    struct { float* out; int64_t part, n; } job[kLoraRecords];
+    half8* operand[2];                  // of g, of h: [chunk][ld / 16][hi, lo][64 lanes]
+    int32_t* exponent[2];               // [chunk]
+    int64_t split_stride;
+    int32_t ld, splits, h_ld, n_jobs, chunk_first, side_first;   // side_first = 1: only h
+    LoraPrepJob job[kLoraRecords];
 };
 
-// `columns`: tokens of a tile (16: records are tiles; 64: records are jobs).  max_rank: the largest rank of the records.
+// side 0: dA [r][F] = sum over a job's tokens of g[token][r] x[token][f];  side 1: dB [F][r] = scale * sum of dy[token][f] h[token][r]
+struct LoraGradJob {
+    float* out[2];                      // nullptr: not wanted
+    int64_t part;                       // ranks of the jobs before it in `partial`
+    int32_t tenant, count, first, rank, chunk_begin;
+};
+struct LoraGradSide {
+    const uint16_t* d;                  // [T, F]
+    const half8* operand;
+    const int32_t* exponent;
+    const float* scale;                 // dB: device, by tenant; dA: nullptr (g has it)
+    float* partial;                     // [token_splits][part_stride], used where token_splits > 1
+    int64_t F, part_stride;
+};
+struct LoraGradArgs {
+    const int32_t* order;
+    LoraGradSide side[2];
+    int32_t ld, token_splits, n_jobs, accumulate, rank_groups;
+    LoraGradJob job[kLoraRecords - 8];
+};
+constexpr int kLoraGradJobs = kLoraRecords - 8;
+// out (+)= sum over the splits of the partial sums; or zeros (token_splits = 0) for gradients of tenants without a token
+struct LoraReduceArgs {
+    int32_t token_splits, n_jobs, accumulate;
+    struct { float* out; const float* partial; int64_t part_stride, n; } job[kLoraRecords];
+};
+
+// `columns`: tokens of a tile (16: records are tiles; else records are jobs, 64 for the shrink, 32 for the expand).  max_rank: the largest rank of the records.
 hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transposed, int max_rank, hipStream_t st);
 hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int64_t max_F, hipStream_t st);
+// prepares `chunks` chunks from a.chunk_first on, of `sides` sides from a.side_first on
+hipError_t launch_lora_prep(const LoraPrepArgs& a, int chunks, int sides, hipStream_t st);
 hipError_t launch_lora_grad(const LoraGradArgs& a, int max_rank, hipStream_t st);
 hipError_t launch_lora_reduce(const LoraReduceArgs& a, int64_t max_n, hipStream_t st);
 

@@ -14,7 +14,7 @@ namespace {
 using bd::misaligned;
 using bd::overlaps;
 
-constexpr int kFewColumns = 16, kManyColumns = 64;   // tokens of a tile: records are tiles, or jobs
+constexpr int kFewColumns = 16, kShrinkColumns = 64, kExpandColumns = 32;   // tokens of a tile: records are tiles; or jobs, by kernel
 constexpr int64_t kFewTokens = 512;                  // largest batch whose records are tiles
 constexpr int kGradParts = 16;                       // jobs x parts of the tokens of a gradient, where there is more than one part
 
@@ -52,7 +52,8 @@ Batch group(const int32_t* tenant_of_token, int64_t T, int32_t n_tenants) {
 // Fills the records of one kernel's launches and runs them: `per_record` says whether a (job, matrix) takes part, with which
 // weight and rank.
 template <typename Args, typename Weight, typename Launch>
-hipError_t for_records(Args& a, const Batch& b, int64_t T, int n_mats, bool few, Weight weight, Launch launch) {
+hipError_t for_records(Args& a, const Batch& b, int64_t T, int n_mats, int columns, Weight weight, Launch launch) {
+    const bool few = columns == kFewColumns;
     int n = 0, tiles = 0, max_rank = 0;
     auto flush = [&]() -> hipError_t {
         if (n == 0) return hipSuccess;
@@ -95,7 +96,7 @@ hipError_t for_records(Args& a, const Batch& b, int64_t T, int n_mats, bool few,
                 t.rank = (uint16_t)rank;
                 t.mat = (uint16_t)m;
                 ++n;
-                tiles += (j.count + kManyColumns - 1) / kManyColumns;
+                tiles += (j.count + columns - 1) / columns;
                 max_rank = std::max(max_rank, rank);
                 if (n == bd::kLoraRecords)
                     if (const hipError_t e = flush(); e != hipSuccess) return e;
@@ -104,16 +105,15 @@ hipError_t for_records(Args& a, const Batch& b, int64_t T, int n_mats, bool few,
     return flush();
 }
 
-// The workspace: the order of the tokens, then h (or g) as partial sums.
-struct Workspace {
-    int32_t* order;
-    float* h;
-    float* partial;
-};
+// The workspace: the order of the tokens, then h (or g) as partial sums, then what the gradients need.
 size_t order_bytes(int64_t T) { return (size_t)round_up(T * 4, 256); }
 size_t h_bytes(int64_t T, int32_t n_mats, int32_t max_rank) {
     return (size_t)round_up((int64_t)max_splits(T) * n_mats * T * round_up(max_rank, 16) * 4, 256);
 }
+// operands of the gradients: 32 tokens of a job by 16 ranks as hi and lo, for g and for h, and their exponents
+int64_t most_chunks(int64_t T, int32_t n_tenants) { return T / 32 + std::min<int64_t>(T, n_tenants); }
+size_t operand_bytes(int64_t chunks, int32_t max_rank) { return (size_t)(chunks * (round_up(max_rank, 16) / 16) * 2 * 64 * 16); }
+size_t exponent_bytes(int64_t chunks) { return (size_t)round_up(chunks * 4, 256); }
 size_t grad_part_bytes(int64_t out, int64_t in, int32_t max_rank) {
     return (size_t)round_up((int64_t)kGradParts * round_up(max_rank, 16) * (in + out) * 4, 256);
 }
@@ -180,7 +180,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
         return BD_ERR_WORKSPACE;
     // ---- checked: launches from here on ----
     const bool few = T <= kFewTokens;
-    const int columns = few ? kFewColumns : kManyColumns;
+    const int columns = few ? kFewColumns : kShrinkColumns, expand_columns = few ? kFewColumns : kExpandColumns;
     const int32_t* order = nullptr;
     if (!few && !batch.order.empty() && max_rank > 0) {
         if (bd::write_int_table(batch.order, (int32_t*)workspace, st) != hipSuccess) return BD_ERR_DEVICE;
@@ -203,7 +203,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
         s->splits = splits;
         s->split_stride = n_mats * T * ld;
         const hipError_t e = for_records(
-            *s, batch, T, n_mats, few,
+            *s, batch, T, n_mats, columns,
             [&](int m, int32_t tenant, const uint16_t** w, int* rank) {
                 const size_t at = (size_t)m * n_tenants + tenant;
                 *w = a_by[at];
@@ -228,7 +228,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
     x2->splits = splits;
     x2->split_stride = n_mats * T * ld;
     const hipError_t e = for_records(
-        *x2, batch, T, n_mats, few,
+        *x2, batch, T, n_mats, expand_columns,
         [&](int m, int32_t tenant, const uint16_t** w, int* rank) {
             const size_t at = (size_t)m * n_tenants + tenant;
             *w = b_by[at];
@@ -236,7 +236,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
             // without an adapter there is nothing to do where y is y0
             return (out[m] > 0 || (h && h[m])) && (rank_by[at] > 0 || !(y0 && y0[m] == y[m]));
         },
-        [&](int) { return bd::launch_lora_expand(*x2, columns, false, max_out, st); });
+        [&](int) { return bd::launch_lora_expand(*x2, expand_columns, false, max_out, st); });
     return e == hipSuccess ? BD_OK : BD_ERR_DEVICE;
 }
 
@@ -275,11 +275,13 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         const bool da = da_by && da_by[e], db = db_by && db_by[e];
         if (!da && !db) continue;
         if (rank_by[e] < 0 || rank_by[e] > bd::kLoraMaxRank) return BD_ERR_SHAPE;
-        if ((da && misaligned(da_by[e], 16)) || (db && misaligned(db_by[e], 16))) return BD_ERR_ALIGN;
+        if ((da && misaligned(da_by[e], 4)) || (db && misaligned(db_by[e], 4))) return BD_ERR_ALIGN;
         if (!has_tokens[(size_t)e] && accumulate) continue;
         if (da) range(da_by[e], (size_t)rank_by[e] * in * 4, true);
         if (db) range(db_by[e], (size_t)rank_by[e] * out * 4, true);
     }
+    any_da &= in > 0;
+    any_db &= out > 0;
     const bool work = T > 0 && max_rank > 0, want_dx = dx && T > 0 && in > 0;
     if (work) {
         if (out > 0 && (dx || any_da || any_db) && !dy) return BD_ERR_NULL;
@@ -297,11 +299,11 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         if (dx0 != dx) range(dx0, (size_t)T * in * 2, false);
     }
     if (bd::any_alias(ranges)) return BD_ERR_ALIAS;
-    if (work && (!workspace || misaligned(workspace, 256) || workspace_bytes < bd_lora_backward_workspace_bytes(T, out, in, max_rank)))
+    if (work && (!workspace || misaligned(workspace, 256) || workspace_bytes < bd_lora_backward_workspace_bytes(T, out, in, n_tenants, max_rank)))
         return BD_ERR_WORKSPACE;
     // ---- checked: launches from here on ----
     const bool few = T <= kFewTokens;
-    const int columns = few ? kFewColumns : kManyColumns;
+    const int columns = few ? kFewColumns : kShrinkColumns, expand_columns = few ? kFewColumns : kExpandColumns;
     const int64_t ld = round_up(max_rank, 16);
     const int32_t* order = nullptr;
     if (work && !batch.order.empty()) {   // (the gradients' sums run over a job's tokens, for few tokens too)
@@ -309,10 +311,9 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         order = (const int32_t*)workspace;
     }
     float* const g = work ? (float*)((char*)workspace + order_bytes(T)) : nullptr;
-    float* const partial = work ? (float*)((char*)g + h_bytes(T, 1, max_rank)) : nullptr;
     int64_t tiles = 0;
     for (const Job& j : batch.jobs) tiles += (int64_t)(j.count + columns - 1) / columns * ((rank_by[j.tenant] + 15) / 16);
-    const int splits = sum_splits(std::max<int64_t>(tiles, 1), out, T);
+    int splits = sum_splits(std::max<int64_t>(tiles, 1), out, T);
     auto weights_of = [&](const uint16_t* const* by, bool all) {
         return [=](int, int32_t tenant, const uint16_t** w, int* rank) {
             *rank = rank_by[tenant];
@@ -330,8 +331,90 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         s->ld = (int32_t)ld;
         s->splits = splits;
         s->split_stride = T * ld;
-        if (for_records(*s, batch, T, 1, few, weights_of(b_by, false), [&](int rank) { return bd::launch_lora_shrink(*s, columns, true, rank, st); }) != hipSuccess)
+        if (for_records(*s, batch, T, 1, columns, weights_of(b_by, false), [&](int rank) { return bd::launch_lora_shrink(*s, columns, true, rank, st); }) != hipSuccess)
             return BD_ERR_DEVICE;
+    }
+    // ---- g (parts added up) and h as operands of the gradients ----
+    const int64_t chunks_most = most_chunks(T, n_tenants);
+    bd::half8* operand[2] = {nullptr, nullptr};
+    int32_t* exponent[2] = {nullptr, nullptr};
+    float* partial = nullptr;
+    if (work) {
+        char* p = (char*)g + h_bytes(T, 1, max_rank);
+        for (int side = 0; side < 2; ++side, p += operand_bytes(chunks_most, max_rank)) operand[side] = (bd::half8*)p;
+        for (int side = 0; side < 2; ++side, p += exponent_bytes(chunks_most)) exponent[side] = (int32_t*)p;
+        partial = (float*)p;
+    }
+    if (work && (any_da || any_db)) {
+        auto prep = std::make_unique<bd::LoraPrepArgs>();
+        auto args = std::make_unique<bd::LoraGradArgs>();
+        prep->g = g;
+        prep->h = h;
+        prep->order = args->order = order;
+        for (int side = 0; side < 2; ++side) {
+            prep->operand[side] = operand[side];
+            prep->exponent[side] = exponent[side];
+            bd::LoraGradSide& v = args->side[side];
+            v.d = side ? dy : x;
+            v.operand = operand[side];
+            v.exponent = exponent[side];
+            v.scale = side ? scale : nullptr;
+            v.F = side ? (any_db ? out : 0) : (any_da ? in : 0);
+            v.partial = partial + (side ? (int64_t)kGradParts * ld * in : 0);
+        }
+        prep->split_stride = T * ld;
+        prep->ld = args->ld = (int32_t)ld;
+        prep->splits = splits;
+        prep->h_ld = h_ld;
+        prep->side_first = any_da ? 0 : 1;
+        args->accumulate = accumulate ? 1 : 0;
+        std::vector<Job> wanted;   // (all with a rank: the sum of g's parts is the expand's input too)
+        for (const Job& j : batch.jobs)
+            if (rank_by[j.tenant] > 0) wanted.push_back(j);
+        int32_t chunk = 0;
+        for (size_t first = 0; first < wanted.size(); first += bd::kLoraGradJobs) {
+            const int n = (int)std::min<size_t>(bd::kLoraGradJobs, wanted.size() - first);
+            int64_t part = 0;
+            int most = 0, longest = 0;
+            prep->chunk_first = chunk;
+            for (int i = 0; i < n; ++i) {
+                const Job& j = wanted[first + (size_t)i];
+                const int rank = rank_by[j.tenant];
+                prep->job[i] = bd::LoraPrepJob{j.first, j.count, rank, chunk};
+                args->job[i] = bd::LoraGradJob{{da_by && in > 0 ? da_by[j.tenant] : nullptr, db_by && out > 0 ? db_by[j.tenant] : nullptr},
+                                               part, j.tenant, j.count, j.first, rank, chunk};
+                chunk += (j.count + 31) / 32;
+                part += rank;
+                most = std::max(most, rank);
+                longest = std::max(longest, (int)j.count);
+            }
+            prep->n_jobs = args->n_jobs = n;
+            if (bd::launch_lora_prep(*prep, chunk - prep->chunk_first, (any_da ? 1 : 0) + (any_db ? 1 : 0), st) != hipSuccess) return BD_ERR_DEVICE;
+            const int64_t groups = n * ((args->side[0].F + bd::kLoraFeatures - 1) / bd::kLoraFeatures + (args->side[1].F + bd::kLoraFeatures - 1) / bd::kLoraFeatures);
+            if (groups == 0) continue;
+            // few workgroups: the tokens of a job in parts of at least 256
+            args->token_splits = (int)std::max<int64_t>(1, std::min({(1024 + groups - 1) / groups, (int64_t)kGradParts / n, (int64_t)longest / 256}));
+            for (int side = 0; side < 2; ++side) args->side[side].part_stride = part * args->side[side].F;
+            if (bd::launch_lora_grad(*args, most, st) != hipSuccess) return BD_ERR_DEVICE;
+            if (args->token_splits == 1) continue;
+            auto sum = std::make_unique<bd::LoraReduceArgs>();   // (token_splits > 1: 8 jobs at most)
+            sum->token_splits = args->token_splits;
+            sum->accumulate = args->accumulate;
+            int64_t max_n = 0;
+            for (int i = 0; i < n; ++i)
+                for (int side = 0; side < 2; ++side) {
+                    const bd::LoraGradSide& v = args->side[side];
+                    if (!args->job[i].out[side]) continue;
+                    auto& r = sum->job[sum->n_jobs++];
+                    r.out = args->job[i].out[side];
+                    r.partial = v.partial + args->job[i].part * v.F;
+                    r.part_stride = v.part_stride;
+                    r.n = args->job[i].rank * v.F;
+                    max_n = std::max(max_n, r.n);
+                }
+            if (sum->n_jobs > 0 && bd::launch_lora_reduce(*sum, max_n, st) != hipSuccess) return BD_ERR_DEVICE;
+        }
+        if (any_da) splits = 1;   // g is whole
     }
     if (want_dx) {
         auto x2 = std::make_unique<bd::LoraExpandArgs>();
@@ -343,63 +426,15 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         x2->ld = (int32_t)ld;
         x2->splits = splits;
         x2->split_stride = T * ld;
-        if (for_records(*x2, batch, T, 1, few, weights_of(a_by, dx0 != dx), [&](int) { return bd::launch_lora_expand(*x2, columns, true, in, st); }) != hipSuccess)
+        if (for_records(*x2, batch, T, 1, expand_columns, weights_of(a_by, dx0 != dx), [&](int) { return bd::launch_lora_expand(*x2, expand_columns, true, in, st); }) != hipSuccess)
             return BD_ERR_DEVICE;
-    }
-    for (int which = 0; which < 2 && work; ++which) {   // dA, then dB
-        float* const* const by = which ? db_by : da_by;
-        const int64_t F = which ? out : in;
-        if (!(which ? any_db : any_da) || F == 0) continue;
-        auto args = std::make_unique<bd::LoraGradArgs>();
-        auto sum = std::make_unique<bd::LoraReduceArgs>();
-        args->d = which ? dy : x;
-        args->w = which ? h : g;
-        args->scale = which ? scale : nullptr;
-        args->order = order;
-        args->F = F;
-        args->w_ld = which ? h_ld : (int32_t)ld;
-        args->w_splits = which ? 1 : splits;
-        args->w_split_stride = T * ld;
-        args->accumulate = sum->accumulate = accumulate ? 1 : 0;
-        args->w_by_token = which;
-        args->rank_major = !which;
-        args->partial = partial + (which ? (int64_t)kGradParts * ld * in : 0);
-        sum->partial = args->partial;
-        std::vector<Job> wanted;
-        for (const Job& j : batch.jobs)
-            if (rank_by[j.tenant] > 0 && by[j.tenant]) wanted.push_back(j);
-        for (size_t first = 0; first < wanted.size(); first += bd::kLoraRecords) {
-            const int n = (int)std::min<size_t>(bd::kLoraRecords, wanted.size() - first);
-            int64_t part = 0, max_n = 0;
-            int most = 0, longest = 0;
-            for (int i = 0; i < n; ++i) {
-                const Job& j = wanted[first + (size_t)i];
-                const int rank = rank_by[j.tenant];
-                args->job[i] = bd::LoraGradJob{by[j.tenant], part, j.tenant, j.count, j.first, rank};
-                sum->job[i].out = by[j.tenant];
-                sum->job[i].part = part;
-                sum->job[i].n = rank * F;
-                part += rank * F;
-                max_n = std::max(max_n, rank * F);
-                most = std::max(most, rank);
-                longest = std::max(longest, (int)j.count);
-            }
-            const int64_t groups = n * ((F + bd::kLoraFeatures - 1) / bd::kLoraFeatures);
-            args->n_jobs = sum->n_jobs = n;
-            // few workgroups: the tokens of a job in parts of at least 256
-            args->token_splits = sum->token_splits =
-                (int)std::max<int64_t>(1, std::min({(512 + groups - 1) / groups, (int64_t)kGradParts / n, (int64_t)longest / 256}));
-            args->part_stride = sum->part_stride = part;
-            if (bd::launch_lora_grad(*args, most, st) != hipSuccess) return BD_ERR_DEVICE;
-            if (args->token_splits > 1 && bd::launch_lora_reduce(*sum, max_n, st) != hipSuccess) return BD_ERR_DEVICE;
-        }
     }
     if (!accumulate) {   // gradients of adapters that no token used
         auto zero = std::make_unique<bd::LoraReduceArgs>();
         int n = 0;
         int64_t max_n = 0;
         auto flush = [&]() {
-            zero->n_jobs = n;
+            zero->n_jobs = n;   // (token_splits = 0: the sum of nothing)
             const bool ok = n == 0 || bd::launch_lora_reduce(*zero, max_n, st) == hipSuccess;
             n = 0;
             max_n = 0;
@@ -431,9 +466,10 @@ size_t bd_lora_workspace_bytes(int64_t T, int32_t n_mats, int32_t max_rank) {
     return order_bytes(T) + h_bytes(T, n_mats, max_rank);
 }
 
-size_t bd_lora_backward_workspace_bytes(int64_t T, int64_t out, int64_t in, int32_t max_rank) {
-    if (T < 1 || !sizes_ok(T, out, in, 0) || max_rank < 1 || max_rank > bd::kLoraMaxRank) return 0;
-    return order_bytes(T) + h_bytes(T, 1, max_rank) + grad_part_bytes(out, in, max_rank);
+size_t bd_lora_backward_workspace_bytes(int64_t T, int64_t out, int64_t in, int32_t n_tenants, int32_t max_rank) {
+    if (T < 1 || !sizes_ok(T, out, in, n_tenants) || n_tenants < 1 || max_rank < 1 || max_rank > bd::kLoraMaxRank) return 0;
+    const int64_t chunks = most_chunks(T, n_tenants);
+    return order_bytes(T) + h_bytes(T, 1, max_rank) + 2 * (operand_bytes(chunks, max_rank) + exponent_bytes(chunks)) + grad_part_bytes(out, in, max_rank);
 }
 
 // (what the standard library throws here is a lack of host memory)

@@ -13,6 +13,8 @@
 //
 // v_mfma_f32_16x16x32_f16: lane l = (r, g) = (l % 16, l / 16) supplies row r, elements 8 g .. 8 g + 7 of either operand; result
 // register i of lane (n, q) is element (4 q + i, n).
+#include <algorithm>
+
 #include "bd_device.h"
 #include "bd_lora.h"
 
@@ -103,10 +105,30 @@ __device__ __forceinline__ int token_of(const Args& a, const Where& u, int colum
 
 constexpr int kShrinkThreads = kLoraShrinkWaves * kWave;
 
+// A wavefront's own piece of LDS, 32 rows of 16 RT ranks of B (B [K, rank] has the sum's index outside): stored as rows, read back
+// as matrix-core operands by the transposing read, which gives lane c of 16 the column c of the 4 x 16 block that the 16 lanes'
+// addresses cover.  The pitch of 8 more keeps rows on different banks.
+template <int RT>
+struct Stage {
+    static constexpr int kPitch = 16 * RT + 8;
+    _Float16 row[32][kPitch];
+
+    __device__ __forceinline__ half8 operand(int r, int lane) const {
+        typedef short s4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s4 lds4;
+        const int g = lane >> 4, c = lane & 15;
+        const _Float16* const p = &row[8 * g + (c >> 2)][16 * r + 4 * (c & 3)];
+        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 4 * kPitch));
+        half8 v;
+        __builtin_memcpy(&v, &lo, 8);
+        __builtin_memcpy((char*)&v + 8, &hi, 8);
+        return v;
+    }
+};
+
 // h = A x or g = s B^T dy of one tile, 16 RT ranks and one part of the sum.  The wavefronts divide the part among them; each
-// reads its operands straight into matrix-core order (a row's 64 bytes per instruction), the eight sums meet in LDS.
-// Rows of A beyond the rank and columns without a token repeat the first: rows and columns do not mix, and what they give is
-// not kept.
+// reads x (and A) straight into matrix-core order (a row's 64 bytes per instruction), the eight sums meet in LDS.
+// Ranks and columns beyond the last repeat others or hold anything: rows and columns do not mix, and what they give is not kept.
 template <bool TR, int NT, int RT>
 __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraShrinkArgs a) {
     const Where u = find_tile<NT>(a, blockIdx.x);
@@ -119,78 +141,92 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
         const int c = 16 * n + m;
         row[n] = a.src + (int64_t)token_of<NT>(a, u, c < u.count ? c : 0) * a.K + 8 * g;
     }
+    constexpr size_t kSums = sizeof(float4v) * kLoraShrinkWaves * NT * kWave, kStages = TR ? sizeof(Stage<RT>) * kLoraShrinkWaves : 0;
+    __shared__ __align__(16) char lds[kSums > kStages ? kSums : kStages];
+    Stage<RT>& stage = ((Stage<RT>*)lds)[wave];
+    // backward: the lane's 16-byte pieces of 32 rows of B, where rows are whole pieces; else element by element
+    const int width = min(16 * RT, u.rank - 16 * rt0);
+    const bool pieces = u.rank % 8 == 0;
+    int piece_row[RT], piece_col[RT];
     const uint16_t* wrow[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int rank = 16 * (rt0 + r) + m < u.rank ? 16 * (rt0 + r) + m : 0;
-        wrow[r] = TR ? u.w + (int64_t)8 * g * u.rank + rank : u.w + (int64_t)rank * a.K + 8 * g;
+        if constexpr (TR) {
+            const int at = lane + kWave * r, per_row = width / 8;
+            piece_row[r] = pieces ? at / per_row : 32;   // 32: none
+            piece_col[r] = pieces ? 8 * (at % per_row) : 0;
+            wrow[r] = u.w + (int64_t)piece_row[r] * u.rank + 16 * rt0 + piece_col[r];
+        } else {
+            const int rank = 16 * (rt0 + r) + m < u.rank ? 16 * (rt0 + r) + m : 0;
+            wrow[r] = u.w + (int64_t)rank * a.K + 8 * g;
+        }
     }
     float4v acc[RT][NT] = {};
     const int64_t steps = (a.K + 31) / 32, parts = (int64_t)a.splits * kLoraShrinkWaves, part = (int64_t)blockIdx.y * kLoraShrinkWaves + wave;
     const int64_t s0 = steps * part / parts, s1 = steps * (part + 1) / parts;
     const int64_t whole = a.K / 32 < s1 ? a.K / 32 : s1;   // steps of 32 elements; a last one of fewer is the backward pass's only
-    auto steps_at = [&](auto count, int64_t s) {   // `count` steps: all their loads, then their products
+    auto steps_at = [&](auto count, auto ragged, int64_t s) {   // `count` steps: all their loads, then their products
         constexpr int C = decltype(count)::value;
+        constexpr bool kRagged = decltype(ragged)::value;
+        const int64_t left = a.K - 32 * s;                  // (ragged: below 32, one step)
         half8 xv[C][NT], wv[C][RT];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) xv[c][n] = load8(row[n] + 32 * (s + c));
+            for (int n = 0; n < NT; ++n) xv[c][n] = kRagged ? load8_upto(row[n] + 32 * s, left - 8 * g) : load8(row[n] + 32 * (s + c));
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                if constexpr (TR) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) wv[c][r][i] = __builtin_bit_cast(_Float16, wrow[r][(32 * (s + c) + i) * u.rank]);
-                } else {
+                if constexpr (TR)
+                    wv[c][r] = piece_row[r] < (kRagged ? (int)left : 32) ? load8(wrow[r] + 32 * (s + c) * u.rank) : half8{};
+                else
                     wv[c][r] = load8(wrow[r] + 32 * (s + c));
-                }
             }
         }
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+        for (int c = 0; c < C; ++c) {
+            if constexpr (TR) {
+                if (pieces) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
+                    for (int r = 0; r < RT; ++r)
+                        if (piece_row[r] < 32) *(half8*)&stage.row[piece_row[r]][piece_col[r]] = wv[c][r];
+                } else {
+                    for (int at = lane; at < 32 * width; at += kWave) {
+                        const int k = at / width, rank = at % width;
+                        stage.row[k][rank] = !kRagged || k < left ? *(const _Float16*)(u.w + (32 * (s + c) + k) * u.rank + 16 * rt0 + rank) : (_Float16)0.0f;
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
 #pragma unroll
-                for (int n = 0; n < NT; ++n) acc[r][n] = mfma(wv[c][r], xv[c][n], acc[r][n]);
+            for (int r = 0; r < RT; ++r) {
+                const half8 w = TR ? stage.operand(r, lane) : wv[c][r];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[r][n] = mfma(w, xv[c][n], acc[r][n]);
+            }
+            if constexpr (TR) __builtin_amdgcn_wave_barrier();
+        }
     };
     constexpr int kAtOnce = NT * RT == 1 ? 8 : NT + RT <= 5 ? 4 : 2;   // what the registers hold
     int64_t s = s0;
-    for (; s + kAtOnce <= whole; s += kAtOnce) steps_at(std::integral_constant<int, kAtOnce>{}, s);
-    for (; s < whole; ++s) steps_at(std::integral_constant<int, 1>{}, s);
-    if (TR && whole < s1 && s0 < s1) {
-        s = s1 - 1;
-        const int64_t left = a.K - 32 * s - 8 * g;
-        half8 xv[NT], wv[RT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) xv[n] = load8_upto(row[n] + 32 * s, left);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            wv[r] = half8{};
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < left) wv[r][i] = __builtin_bit_cast(_Float16, wrow[r][(32 * s + i) * u.rank]);
-        }
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) acc[r][n] = mfma(wv[r], xv[n], acc[r][n]);
-    }
-    __shared__ float4v part_sum[kLoraShrinkWaves][NT][kWave];
+    for (; s + kAtOnce <= whole; s += kAtOnce) steps_at(std::integral_constant<int, kAtOnce>{}, std::false_type{}, s);
+    for (; s < whole; ++s) steps_at(std::integral_constant<int, 1>{}, std::false_type{}, s);
+    if (TR && s < s1) steps_at(std::integral_constant<int, 1>{}, std::true_type{}, s);
     const float scale = TR ? a.scale[u.tenant] : 1.0f;
     float* const dst = a.h + (int64_t)blockIdx.y * a.split_stride;
+    auto* const sum = (float4v(*)[NT][kWave])lds;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         if (16 * (rt0 + r) >= u.rank) continue;   // (of the whole workgroup)
-        if (r > 0) __syncthreads();
+        if (TR || r > 0) __syncthreads();
 #pragma unroll
-        for (int n = 0; n < NT; ++n) part_sum[wave][n][lane] = acc[r][n];
+        for (int n = 0; n < NT; ++n) sum[wave][n][lane] = acc[r][n];
         __syncthreads();
         for (int t = threadIdx.x; t < NT * kWave; t += kShrinkThreads) {
             const int n = t / kWave, l = t & (kWave - 1), c = 16 * n + (l & 15), rank = 16 * (rt0 + r) + 4 * (l >> 4);
             if (c >= u.count) continue;
-            float4v v = part_sum[0][n][l];
+            float4v v = sum[0][n][l];
 #pragma unroll
-            for (int w = 1; w < kLoraShrinkWaves; ++w) v += part_sum[w][n][l];
+            for (int w = 1; w < kLoraShrinkWaves; ++w) v += sum[w][n][l];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = rank + i < u.rank ? v[i] * scale : 0.0f;
             *(float4v*)(dst + (int64_t)(u.hrow + c) * a.ld + rank) = v;
@@ -201,21 +237,62 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
 constexpr int kExpandThreads = kLoraExpandWaves * kWave;
 constexpr int kExpandRanks = 128;   // ranks whose hi and lo are in LDS at a time
 
-// y = y0 + s B h, or dx = dx0 + A^T g, of one tile by 512 features.  h comes in as `splits` partial sums.  Feature 8 m + j of a
-// wavefront's 128 is row m of its MFMA j, so that a lane ends up with 8 neighbours of a token's row in the 8 accumulators: one
-// 16-byte load of y0 and one such store for each.  The 32 elements of an MFMA's sum are 16 ranks, hi in lane groups 0 and 1 and
-// lo in 2 and 3, both with the same weights.
+// y = y0 + s B h, or dx = dx0 + A^T g, of one tile by 512 features.  h comes in as `splits` partial sums.  Rows of a result are
+// tokens, columns features: feature 8 n + j of a wavefront's 128 is column n of its MFMA j, so that a lane ends up with 8
+// neighbours of a token's row in its 8 accumulators, and 16 lanes with 256 bytes of the row: one load of y0 and one store for
+// each.  The 32 elements of an MFMA's sum are 16 ranks, hi in lane groups 0 and 1 and lo in 2 and 3, both with the same weights.
+// y0 and the first weights are asked for before h is prepared: three waits for memory become one.
 template <bool TR, int NT>
 __global__ __launch_bounds__(kExpandThreads) void lora_expand_kernel(const LoraExpandArgs a) {
     constexpr int kTokens = 16 * NT, kPer = kExpandThreads / kTokens;   // threads per token while h is prepared
     constexpr int kPitch = kExpandRanks + 8;
     __shared__ __align__(16) _Float16 hi[kTokens][kPitch], lo[kTokens][kPitch];
-    __shared__ int exponent[kTokens];
+    __shared__ float unit[kTokens];
     const Where u = find_tile<NT>(a, blockIdx.x);
     const int64_t F = a.F[u.mat];
     if (blockIdx.y > 0 && (int64_t)blockIdx.y * kLoraExpandWaves * kLoraFeatures >= F) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
     const int padded = (u.rank + 15) & ~15;
+    const int64_t f0 = ((int64_t)blockIdx.y * kLoraExpandWaves + wave) * kLoraFeatures, f = f0 + 8 * m;
+    const bool active = f0 < F, inside = f0 + kLoraFeatures <= F;
+
+    int64_t at[NT][4];   // the rows of y that the lane's results belong to: token 16 n + 4 g + i
+    half8 before[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = 16 * n + 4 * g + i;
+            at[n][i] = (int64_t)token_of<NT>(a, u, c < u.count ? c : 0) * F + f;
+        }
+    const uint16_t* const y0 = active ? a.y0[u.mat] : nullptr;
+    if (y0 && inside) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) before[n][i] = load8(y0 + at[n][i]);
+    } else {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) before[n][i] = y0 && f < F ? load8_upto(y0 + at[n][i], F - f) : half8{};
+    }
+    half8 wv[8];   // forward: the weights of 16 ranks; backward: 8 ranks' rows of A, still to be turned
+    auto load_weights = [&](int r) {
+        const int rank = r + 8 * (g & 1), left = u.rank - rank;
+        if constexpr (TR) {
+            const int64_t col = f <= F - 8 ? f : F - 8;   // (F = in, a multiple of 32)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) wv[i] = i < left ? load8(u.w + (int64_t)(rank + i) * F + col) : half8{};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int64_t row = f + j < F ? f + j : F - 1;
+                wv[j] = load8_upto(u.w + row * u.rank + rank, left);
+            }
+        }
+    };
+    if (active && padded > 0) load_weights(0);
 
     const int c = threadIdx.x / kPer, sub = threadIdx.x % kPer;   // the token whose h this thread prepares
     const bool real = c < u.count;
@@ -238,11 +315,9 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_kernel(const LoraE
 #pragma unroll
     for (int d = kPer / 2; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
     const int e = group_exponent(top);
-    if (sub == 0) exponent[c] = e;
+    if (sub == 0) unit[c] = power_of_two(e);
     const float down = power_of_two(-e);
 
-    const int64_t f0 = ((int64_t)blockIdx.y * kLoraExpandWaves + wave) * kLoraFeatures;
-    const bool active = f0 < F;
     float4v acc[8][NT] = {};
     for (int r0 = 0; r0 < padded; r0 += kExpandRanks) {
         const int ranks = min(kExpandRanks, padded - r0);
@@ -260,121 +335,189 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_kernel(const LoraE
         __syncthreads();
         if (!active) continue;
         for (int rc = 0; rc < ranks; rc += 16) {
-            half8 wv[8];
-            const int rank = r0 + rc + 8 * (g & 1), left = u.rank - rank;
+            half8 cols[8];
             if constexpr (TR) {
-                half8 rows[8];
-                const int64_t f = f0 + 8 * m <= F - 8 ? f0 + 8 * m : F - 8;   // (F = in, a multiple of 32)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) rows[i] = i < left ? load8(u.w + (int64_t)(rank + i) * F + f) : half8{};
-                transpose8(rows, wv);
+                transpose8(wv, cols);
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int64_t f = f0 + 8 * m + j < F ? f0 + 8 * m + j : F - 1;
-                    wv[j] = load8_upto(u.w + f * u.rank + rank, left);
-                }
+                for (int j = 0; j < 8; ++j) cols[j] = wv[j];
             }
+            if (r0 + rc + 16 < padded) load_weights(r0 + rc + 16);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const half8 hv = *(const half8*)(g < 2 ? &hi[16 * n + m][rc + 8 * g] : &lo[16 * n + m][rc + 8 * (g - 2)]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j][n] = mfma(wv[j], hv, acc[j][n]);
+                for (int j = 0; j < 8; ++j) acc[j][n] = mfma(hv, cols[j], acc[j][n]);
             }
         }
     }
-    if (padded == 0) __syncthreads();   // `exponent`
+    if (padded == 0) __syncthreads();   // `unit`
     if (!active) return;
     const float scale = TR || u.rank == 0 ? 1.0f : a.scale[u.mat][u.tenant];
+    uint16_t* const y = a.y[u.mat];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int col = 16 * n + m;
-        if (col >= u.count) continue;
-        const int64_t at = (int64_t)token_of<NT>(a, u, col) * F;
-        const uint16_t* const y0 = a.y0[u.mat] ? a.y0[u.mat] + at : nullptr;
-        uint16_t* const y = a.y[u.mat] + at;
-        const float up = power_of_two(exponent[col]);
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t f = f0 + 32 * g + 8 * i;
-            if (f >= F) continue;
-            const half8 before = y0 ? load8_upto(y0 + f, F - f) : half8{};
+            const int col = 16 * n + 4 * g + i;
+            if (col >= u.count || f >= F) continue;
+            const float up = unit[col];
             half8 v;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (_Float16)((float)before[j] + scale * (acc[j][n][i] * up));
+            for (int j = 0; j < 8; ++j) v[j] = (_Float16)((float)before[n][i][j] + scale * (acc[j][n][i] * up));
             if (F - f >= 8) {
-                __builtin_memcpy(y + f, &v, 16);
+                __builtin_memcpy(y + at[n][i], &v, 16);
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (j < F - f) *(_Float16*)(y + f + j) = v[j];
+                    if (j < F - f) *(_Float16*)(y + at[n][i] + j) = v[j];
             }
         }
+}
+
+constexpr int kPrepThreads = 256;
+
+// The second operand of the gradients, once for all their workgroups: 32 tokens' g (or h) as hi and lo in matrix-core order, one
+// exponent for the 32.  Lane (n, q) holds rank n of its 16, tokens 8 q .. 8 q + 7, in 16 bytes.  Where g came in parts their sum
+// takes the first part's place.
+__global__ __launch_bounds__(kPrepThreads) void lora_prep_kernel(const LoraPrepArgs a) {
+    int j = 0;
+    while (j + 1 < a.n_jobs && a.job[j + 1].chunk_begin <= (int)blockIdx.x + a.chunk_first) ++j;
+    const LoraPrepJob& job = a.job[j];
+    const bool of_h = blockIdx.y + a.side_first == 1;
+    const int chunk = blockIdx.x + a.chunk_first, t0 = (chunk - job.chunk_begin) * 32, rank_all = job.rank, tiles = (rank_all + 15) / 16;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = lane & 15, q = lane >> 4;
+    constexpr int kMine = kLoraMaxRank / 16 / (kPrepThreads / kWave);   // rank tiles of a wavefront
+    float v[kMine][8];
+    float top = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+        const int rt = wave + k * (kPrepThreads / kWave), rank = 16 * rt + n;
+        if (rt >= tiles) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int t = t0 + 8 * q + i;
+            v[k][i] = 0.0f;
+            if (t >= job.count || rank >= rank_all) continue;
+            const int p = job.first + t;
+            if (of_h) {
+                v[k][i] = a.h[(int64_t)(a.order ? a.order[p] : p) * a.h_ld + rank];
+            } else {
+                float* const at = a.g + (int64_t)p * a.ld + rank;
+                v[k][i] = at[0];
+                for (int s = 1; s < a.splits; ++s) v[k][i] += at[s * a.split_stride];
+                if (a.splits > 1) at[0] = v[k][i];
+            }
+            top = fmaxf(top, finite_abs(v[k][i]));
+        }
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
+    __shared__ float tops[kPrepThreads / kWave];
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kPrepThreads / kWave; ++w) top = fmaxf(top, tops[w]);
+    const int e = group_exponent(top);
+    if (threadIdx.x == 0) a.exponent[of_h][chunk] = e;
+    const float down = power_of_two(-e);
+    half8* const out = a.operand[of_h] + (int64_t)chunk * (a.ld / 16) * 2 * kWave;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+        const int rt = wave + k * (kPrepThreads / kWave);
+        if (rt >= tiles) continue;
+        half8 hi, lo;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            _Float16 h, l;
+            split_half(v[k][i], down, &h, &l);
+            hi[i] = h;
+            lo[i] = l;
+        }
+        out[(2 * rt) * kWave + lane] = hi;
+        out[(2 * rt + 1) * kWave + lane] = lo;
     }
 }
 
 constexpr int kGradThreads = kLoraGradWaves * kWave;
 
 // dA or dB of one job: 128 features by 16 RT ranks, summed over one part of the job's tokens.  The tokens are the sum's index, so
-// both operands want 8 tokens of one feature (rank) in a lane: a lane loads 16 bytes of 8 tokens' rows (256 bytes of a row per
-// instruction) and turns the 8 x 8 block in its registers.  The wavefronts divide the tokens and meet in LDS.
+// both operands want 8 tokens of one feature (rank) in a lane: the second comes prepared, of x (dy) a lane loads 16 bytes of 8
+// tokens' rows (256 bytes of a row per instruction) and turns the 8 x 8 block in its registers.  The wavefronts divide the tokens
+// and meet in LDS.  The sums are kept in units of the present 32 tokens' exponent; tokens whose largest value is 2^-64 of the
+// largest so far are below what binary32 would keep of them.
 template <int RT>
 __global__ __launch_bounds__(kGradThreads) void lora_grad_kernel(const LoraGradArgs a) {
+    const int which = (int)blockIdx.z / a.rank_groups, rt0 = (int)blockIdx.z % a.rank_groups * RT;
+    const LoraGradSide& side = a.side[which];
     const LoraGradJob& job = a.job[blockIdx.y / a.token_splits];
-    const int split = blockIdx.y % a.token_splits, rt0 = blockIdx.z * RT, rank_all = job.rank, count = job.count, first = job.first;
-    if (16 * rt0 >= rank_all) return;
+    const int split = blockIdx.y % a.token_splits, rank_all = job.rank, count = job.count, first = job.first;
+    float* const result = job.out[which];
+    const int64_t F = side.F, f0 = (int64_t)blockIdx.x * kLoraFeatures;
+    if (!result || 16 * rt0 >= rank_all || f0 >= F) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
-    const int64_t F = a.F, f0 = (int64_t)blockIdx.x * kLoraFeatures, fl = f0 + 8 * m;
+    const int64_t fl = f0 + 8 * m;
     const int steps = (count + 31) / 32, parts = a.token_splits * kLoraGradWaves, part = split * kLoraGradWaves + wave;
     const int s0 = (int)((int64_t)steps * part / parts), s1 = (int)((int64_t)steps * (part + 1) / parts);
-    auto token_at = [&](int i) { return a.order ? a.order[first + i] : first + i; };
-    auto weight = [&](int i, int rank) {   // w of the job's token i; 0 where there is none
-        if (i >= count || rank >= rank_all) return 0.0f;
-        if (a.w_by_token) return a.w[(int64_t)token_at(i) * a.w_ld + rank];
-        const float* const p = a.w + (int64_t)(first + i) * a.w_ld + rank;
-        float v = p[0];
-        for (int s = 1; s < a.w_splits; ++s) v += p[s * a.w_split_stride];
-        return v;
-    };
-    float top = 0.0f;
-    for (int s = s0; s < s1; ++s)
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(weight(32 * s + 8 * g + i, 16 * (rt0 + r) + m)));
-#pragma unroll
-    for (int d = 32; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
-    const int e = group_exponent(top);
-    const float down = power_of_two(-e), up = power_of_two(e);
-
-    float4v acc[8][RT] = {};
-    for (int s = s0; s < s1; ++s) {
-        half8 rows[8], dv[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int t = 32 * s + 8 * g + i;
-            rows[i] = t < count && fl < F ? load8_upto(a.d + (int64_t)token_at(t) * F + fl, F - fl) : half8{};
-        }
-        transpose8(rows, dv);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            half8 hi, lo;
+    const bool inside = f0 + kLoraFeatures <= F;
+    half8 rows[8];
+    auto load_rows = [&](int s) {
+        const int t0 = 32 * s + 8 * g;
+        if (inside && 32 * s + 32 <= count) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                _Float16 h, l;
-                split_half(weight(32 * s + 8 * g + i, 16 * (rt0 + r) + m), down, &h, &l);
-                hi[i] = h;
-                lo[i] = l;
+                const int p = first + t0 + i;
+                rows[i] = load8(side.d + (int64_t)(a.order ? a.order[p] : p) * F + fl);
             }
+        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j][r] = mfma(dv[j], hi, acc[j][r]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j][r] = mfma(dv[j], lo, acc[j][r]);
+            for (int i = 0; i < 8; ++i) {
+                const int p = first + t0 + i;
+                rows[i] = t0 + i < count && fl < F ? load8_upto(side.d + (int64_t)(a.order ? a.order[p] : p) * F + fl, F - fl) : half8{};
+            }
         }
+    };
+    float4v acc[8][RT] = {};
+    int e = -200, largest = -200;   // none yet
+    if (s0 < s1) load_rows(s0);
+    for (int s = s0; s < s1; ++s) {
+        const int chunk = job.chunk_begin + s, now = side.exponent[chunk];
+        const half8* const op = side.operand + ((int64_t)chunk * (a.ld / 16) + rt0) * 2 * kWave + lane;
+        half8 hi[RT], lo[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+            if (16 * (rt0 + r) < rank_all) {
+                hi[r] = op[2 * r * kWave];
+                lo[r] = op[(2 * r + 1) * kWave];
+            }
+        half8 dv[8];
+        transpose8(rows, dv);
+        if (s + 1 < s1) load_rows(s + 1);
+        if (now < largest - 64) continue;
+        largest = max(largest, now);
+        if (now != e) {
+            if (e > -200) {
+                const float f = e - now < -126 ? 0.0f : power_of_two(e - now);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) acc[j][r] *= f;
+            }
+            e = now;
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+            if (16 * (rt0 + r) < rank_all) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j][r] = mfma(dv[j], hi[r], acc[j][r]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j][r] = mfma(dv[j], lo[r], acc[j][r]);
+            }
     }
+    const float up = e > -200 ? power_of_two(e) : 0.0f;
     __shared__ float sum[kLoraGradWaves][8][4][kWave];   // [wave][j][i][lane (n, q)] = feature 8 (4 q + i) + j, rank n
-    const float scale = a.scale ? a.scale[job.tenant] : 1.0f;
-    float* const out = a.token_splits > 1 ? a.partial + split * a.part_stride + job.part : job.out;
+    const float scale = side.scale ? side.scale[job.tenant] : 1.0f;
+    float* const out = a.token_splits > 1 ? side.partial + split * side.part_stride + job.part * F : result;
     const bool add = a.accumulate && a.token_splits == 1;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -386,16 +529,16 @@ __global__ __launch_bounds__(kGradThreads) void lora_grad_kernel(const LoraGradA
             for (int i = 0; i < 4; ++i) sum[wave][j][i][lane] = acc[j][r][i] * up;
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 16 * kLoraFeatures / kGradThreads; ++k) {
             const int at = threadIdx.x + k * kGradThreads;   // of 16 x 128
-            const int n = a.rank_major ? at / kLoraFeatures : at & 15, f = a.rank_major ? at % kLoraFeatures : at >> 4;
+            const int n = which == 0 ? at / kLoraFeatures : at & 15, f = which == 0 ? at % kLoraFeatures : at >> 4;
             const int row = f >> 3, j = f & 7, rank = 16 * (rt0 + r) + n;
             if (rank >= rank_all || f0 + f >= F) continue;
             float v = 0.0f;
 #pragma unroll
             for (int w = 0; w < kLoraGradWaves; ++w) v += sum[w][j][row & 3][16 * (row >> 2) + n];
             v *= scale;
-            float* const p = out + (a.rank_major ? (int64_t)rank * F + f0 + f : (f0 + f) * rank_all + rank);
+            float* const p = out + (which == 0 ? (int64_t)rank * F + f0 + f : (f0 + f) * rank_all + rank);
             *p = add ? *p + v : v;
         }
     }
@@ -406,14 +549,14 @@ __global__ __launch_bounds__(256) void lora_reduce_kernel(const LoraReduceArgs a
     const auto& job = a.job[blockIdx.y];
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < job.n; i += (int64_t)gridDim.x * 256) {
         float v = 0.0f;
-        for (int s = 0; a.partial && s < a.token_splits; ++s) v += a.partial[s * a.part_stride + job.part + i];
+        for (int s = 0; s < a.token_splits; ++s) v += job.partial[s * job.part_stride + i];
         job.out[i] = a.accumulate ? job.out[i] + v : v;
     }
 }
 
 }  // namespace
 
-static_assert(sizeof(LoraShrinkArgs) <= 4096 && sizeof(LoraExpandArgs) <= 4096 && sizeof(LoraGradArgs) <= 4096 && sizeof(LoraReduceArgs) <= 4096,
+static_assert(sizeof(LoraShrinkArgs) <= 4096 && sizeof(LoraExpandArgs) <= 4096 && sizeof(LoraGradArgs) <= 4096 && sizeof(LoraReduceArgs) <= 4096 && sizeof(LoraPrepArgs) <= 4096,
               "kernel arguments");
 
 hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transposed, int max_rank, hipStream_t st) {
@@ -437,18 +580,26 @@ hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transpo
         return hipGetLastError();
     };
     if (columns == 16) return transposed ? go(lora_expand_kernel<true, 1>) : go(lora_expand_kernel<false, 1>);
-    return transposed ? go(lora_expand_kernel<true, 4>) : go(lora_expand_kernel<false, 4>);
+    return transposed ? go(lora_expand_kernel<true, 2>) : go(lora_expand_kernel<false, 2>);
+}
+
+hipError_t launch_lora_prep(const LoraPrepArgs& a, int chunks, int sides, hipStream_t st) {
+    if (a.n_jobs < 1 || chunks < 1 || sides < 1) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(lora_prep_kernel, dim3((unsigned)chunks, (unsigned)sides), dim3(kPrepThreads), 0, st, a);
+    return hipGetLastError();
 }
 
 hipError_t launch_lora_grad(const LoraGradArgs& a, int max_rank, hipStream_t st) {
-    const int rank_tiles = (max_rank + 15) / 16;
-    const int64_t groups = (a.F + kLoraFeatures - 1) / kLoraFeatures;
+    const int rank_tiles = (max_rank + 15) / 16, RT = rank_tiles >= 3 ? 4 : rank_tiles;
+    const int64_t F = std::max(a.side[0].F, a.side[1].F), groups = (F + kLoraFeatures - 1) / kLoraFeatures;
     if (a.n_jobs < 1 || rank_tiles < 1 || groups < 1 || a.token_splits < 1) return hipErrorInvalidValue;
-    auto go = [&](auto kernel, int RT) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)(a.n_jobs * a.token_splits), (unsigned)((rank_tiles + RT - 1) / RT)), dim3(kGradThreads), 0, st, a);
+    LoraGradArgs b = a;
+    b.rank_groups = (rank_tiles + RT - 1) / RT;
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)(b.n_jobs * b.token_splits), (unsigned)(2 * b.rank_groups)), dim3(kGradThreads), 0, st, b);
         return hipGetLastError();
     };
-    return rank_tiles == 1 ? go(lora_grad_kernel<1>, 1) : rank_tiles == 2 ? go(lora_grad_kernel<2>, 2) : go(lora_grad_kernel<4>, 4);
+    return RT == 1 ? go(lora_grad_kernel<1>) : RT == 2 ? go(lora_grad_kernel<2>) : go(lora_grad_kernel<4>);
 }
 
 hipError_t launch_lora_reduce(const LoraReduceArgs& a, int64_t max_n, hipStream_t st) {

@@ -310,7 +310,7 @@ def test_replayed_from_a_graph(T, order):
     y, dx, h = torch.empty_like(y0), torch.empty_like(x), torch.zeros((T, 33), dtype=torch.float32, device=DEV)
     da, db = ([torch.empty(w.shape, dtype=torch.float32, device=DEV) if w is not None else None for w in ws] for ws in (a, b))
     grads = bd.LoraGrads(table, da, db)
-    ws = [bd.new_workspace(bd.lora_workspace_bytes(T, 1, 33), DEV), bd.new_workspace(bd.lora_backward_workspace_bytes(T, out, inn, 33), DEV)]
+    ws = [bd.new_workspace(bd.lora_workspace_bytes(T, 1, 33), DEV), bd.new_workspace(bd.lora_backward_workspace_bytes(T, out, inn, 4, 33), DEV)]
 
     def run():
         bd.lora_multitenant(x, table, tok, y0=y0, y=y, h=h, workspace=ws[0])

@@ -33,9 +33,10 @@ def test_workspace_sizes(bd):
     assert f(100, 3, 17) == 512 + 8 * 3 * 100 * 32 * 4
     assert f(65535, 1, 256) == 262144 + 65535 * 256 * 4
     assert f(0, 1, 8) == 0 and f(1, 4, 8) == 0 and f(1, 0, 8) == 0 and f(1, 1, 0) == 0 and f(1, 1, 257) == 0 and f(65536, 1, 1) == 0
-    # and 16 parts of the gradients of one adapter
-    assert b(100, 40, 64, 17) == 512 + 8 * 100 * 32 * 4 + 16 * 32 * (40 + 64) * 4
-    assert b(0, 40, 64, 17) == 0 and b(1, 40, 65, 17) == 0 and b(1, -1, 64, 1) == 0 and b(1, 40, 64, 0) == 0
+    # g and h as operands (2 KB per 16 ranks and chunk of 32 tokens; 3 chunks and one more per tenant), a number per chunk, and 16 parts
+    # of the gradients of one adapter
+    assert b(100, 40, 64, 5, 17) == 512 + 8 * 100 * 32 * 4 + 2 * (8 * 2 * 2048 + 256) + 16 * 32 * (40 + 64) * 4
+    assert b(0, 40, 64, 1, 17) == 0 and b(1, 40, 65, 1, 17) == 0 and b(1, -1, 64, 1, 1) == 0 and b(1, 40, 64, 1, 0) == 0 and b(1, 40, 64, 0, 1) == 0
 
 
 def test_forward_argument_errors(bd):
@@ -83,7 +84,7 @@ def test_forward_group_argument_errors(bd):
 
 def test_backward_argument_errors(bd):
     L = bd.lib()
-    need = bd.lora_backward_workspace_bytes(3, 40, 64, 16)
+    need = bd.lora_backward_workspace_bytes(3, 40, 64, 2, 16)
 
     def call(dy=A, x=2 * A, h=3 * A, ld=16, a=_ptrs(4 * A, 5 * A), b=_ptrs(6 * A, 7 * A), r=_i32(16, 8), s=8 * A, tok=_i32(0, 1, 1), dx0=9 * A,
              dx=10 * A, da=_ptrs(11 * A, 12 * A), db=_ptrs(13 * A, 14 * A), acc=0, T=3, out=40, inn=64, nt=2, ws=15 * A, nb=need):
@@ -95,7 +96,7 @@ def test_backward_argument_errors(bd):
     assert call(a=None) == 1 and call(b=_ptrs(6 * A, None)) == 1 and call(a=_ptrs(None, 5 * A)) == 1
     for name, at in (("dy", 1), ("x", 2), ("dx0", 9), ("dx", 10)):
         assert call(**{name: at * A + 8}) == 3, name
-    assert call(h=3 * A + 2) == 3 and call(s=8 * A + 2) == 3 and call(da=_ptrs(11 * A + 4, 12 * A)) == 3 and call(db=_ptrs(13 * A, 14 * A + 8)) == 3
+    assert call(h=3 * A + 2) == 3 and call(s=8 * A + 2) == 3 and call(da=_ptrs(11 * A + 2, 12 * A)) == 3 and call(db=_ptrs(13 * A, 14 * A + 2)) == 3
     assert call(a=_ptrs(4 * A + 8, 5 * A)) == 3 and call(b=_ptrs(6 * A, 7 * A + 2)) == 3
     assert call(tok=_i32(0, 2, 1)) == 4 and call(tok=_i32(0, -1, 1)) == 4
     assert call(ws=0) == 5 and call(nb=need - 1) == 5 and call(ws=15 * A + 128) == 5
@@ -105,7 +106,7 @@ def test_backward_argument_errors(bd):
     assert call(da=_ptrs(10 * A, 12 * A)) == 8 and call(da=_ptrs(3 * A, 12 * A)) == 8 and call(db=_ptrs(2 * A, 14 * A)) == 8
     # the gradients of a tenant without a token are checked too: they are set to zero
     one = _i32(1, 1, 1)
-    assert call(tok=one, da=_ptrs(12 * A, 12 * A)) == 8 and call(tok=one, r=_i32(300, 8)) == 2 and call(tok=one, da=_ptrs(11 * A + 4, 12 * A)) == 3
+    assert call(tok=one, da=_ptrs(12 * A, 12 * A)) == 8 and call(tok=one, r=_i32(300, 8)) == 2 and call(tok=one, da=_ptrs(11 * A + 2, 12 * A)) == 3
     assert call(T=0, dy=0, x=0, h=0, a=None, b=None, da=None, db=None, ws=0, nb=0, dx=0, dx0=0) == 0
 
 
