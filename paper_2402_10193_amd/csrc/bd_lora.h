@@ -15,6 +15,7 @@ namespace bd {
 constexpr int kLoraMaxRank = 256;
 constexpr int kLoraMaxMats = 3;
 constexpr int kLoraRecords = 64;        // records of one launch
+constexpr int kLoraMaxSplits = 8;       // parts that the shrink's sum may be cut into
 constexpr int kLoraFeatures = 128;      // output features of one wavefront's step: 8 MFMA rows of 16
 constexpr int kLoraShrinkWaves = 8;
 constexpr int kLoraExpandWaves = 4;
@@ -25,13 +26,18 @@ struct LoraTile {                       // few tokens
     int32_t hrow;                       // row of its first token in the workspace's h (or g)
     int32_t tenant;
     uint16_t rank, count, mat, unused;
-    uint16_t col[16];                   // the tokens
+    uint32_t col[8];                    // the tokens, two per word
 };
 struct LoraJob {                        // many tokens
     const uint16_t* w;
-    int32_t hrow, tenant, count, tile_begin;
+    int32_t hrow, tenant, count;
     int32_t first;                      // sorted position of the first token
     uint16_t rank, mat;
+};
+
+struct LoraJobs {
+    int32_t tile_begin[kLoraRecords];   // first tile of every record; behind the last one the largest int
+    LoraJob job[kLoraRecords];
 };
 
 // h[p][j] = sum_k w_j[k] src[token(p)][k], split over `splits` parts of the sum: A x (forward) or B^T dy (backward, w is then
@@ -42,10 +48,10 @@ struct LoraShrinkArgs {
     const int32_t* order;               // sorted position -> token, nullptr: the same (many tokens only)
     float* h;                           // [splits][rows][ld]
     int64_t K, split_stride;            // split_stride = rows * ld
-    int32_t ld, splits, n_records, n_tiles;
+    int32_t ld, splits, n_tiles;
     union {
         LoraTile tile[kLoraRecords];
-        LoraJob job[kLoraRecords];
+        LoraJobs jobs;
     };
 };
 
@@ -59,10 +65,10 @@ struct LoraExpandArgs {
     const float* scale[kLoraMaxMats];   // forward: device, by tenant
     const int32_t* order;
     int64_t F[kLoraMaxMats], split_stride;
-    int32_t ld, splits, n_records, n_tiles, h_ld;
+    int32_t ld, splits, n_tiles, h_ld;
     union {
         LoraTile tile[kLoraRecords];
-        LoraJob job[kLoraRecords];
+        LoraJobs jobs;
     };
 };
 
@@ -110,9 +116,10 @@ struct LoraReduceArgs {
     struct { float* out; const float* partial; int64_t part_stride, n; } job[kLoraRecords];
 };
 
-// `columns`: tokens of a tile (16: records are tiles; else records are jobs, 64 for the shrink, 32 for the expand).  max_rank: the largest rank of the records.
-hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transposed, int max_rank, hipStream_t st);
-hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int64_t max_F, hipStream_t st);
+// `columns`: tokens of a tile (16: records are tiles; else records are jobs, 64 for the shrink, 32 for the expand).  max_rank: the largest rank of the records;
+// odd: some rank is not a multiple of 8 (B's rows are then no whole 16-byte pieces).
+hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transposed, int max_rank, bool odd, hipStream_t st);
+hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int64_t min_F, int64_t max_F, bool odd, hipStream_t st);
 // prepares `chunks` chunks from a.chunk_first on, of `sides` sides from a.side_first on
 hipError_t launch_lora_prep(const LoraPrepArgs& a, int chunks, int sides, hipStream_t st);
 hipError_t launch_lora_grad(const LoraGradArgs& a, int max_rank, hipStream_t st);

@@ -21,7 +21,7 @@ constexpr int kGradParts = 16;                       // jobs x parts of the toke
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // Parts that the shrink's sum may be cut into: few tokens leave compute units idle.
-int max_splits(int64_t T) { return T <= 2048 ? 8 : T <= 8192 ? 4 : T <= 16384 ? 2 : 1; }
+int max_splits(int64_t T) { return T <= 2048 ? bd::kLoraMaxSplits : T <= 8192 ? 4 : T <= 16384 ? 2 : 1; }
 int sum_splits(int64_t groups, int64_t K, int64_t T) {
     const int64_t steps = (K + 31) / 32;   // 8 wavefronts with at least 4 steps each
     const int64_t most = std::min<int64_t>(max_splits(T), steps / (4 * bd::kLoraShrinkWaves)), want = (256 + groups - 1) / groups;
@@ -55,12 +55,14 @@ template <typename Args, typename Weight, typename Launch>
 hipError_t for_records(Args& a, const Batch& b, int64_t T, int n_mats, int columns, Weight weight, Launch launch) {
     const bool few = columns == kFewColumns;
     int n = 0, tiles = 0, max_rank = 0;
+    bool odd = false;
     auto flush = [&]() -> hipError_t {
         if (n == 0) return hipSuccess;
-        a.n_records = n;
         a.n_tiles = tiles;
-        const hipError_t e = launch(max_rank);
+        for (int k = n; k < bd::kLoraRecords && !few; ++k) a.jobs.tile_begin[k] = INT32_MAX;
+        const hipError_t e = launch(max_rank, odd);
         n = tiles = max_rank = 0;
+        odd = false;
         return e;
     };
     for (const Job& j : b.jobs)
@@ -68,6 +70,7 @@ hipError_t for_records(Args& a, const Batch& b, int64_t T, int n_mats, int colum
             const uint16_t* w = nullptr;
             int rank = 0;
             if (!weight(m, j.tenant, &w, &rank)) continue;
+            const bool odd_rank = rank % 8 != 0;
             if (few) {
                 for (int32_t at = 0; at < j.count; at += kFewColumns) {
                     bd::LoraTile& t = a.tile[n];
@@ -78,26 +81,28 @@ hipError_t for_records(Args& a, const Batch& b, int64_t T, int n_mats, int colum
                     t.rank = (uint16_t)rank;
                     t.count = (uint16_t)std::min(kFewColumns, j.count - at);
                     t.mat = (uint16_t)m;
-                    for (int c = 0; c < t.count; ++c) t.col[c] = (uint16_t)b.token(j.first + at + c);
+                    for (int c = 0; c < t.count; ++c) t.col[c >> 1] |= (uint32_t)b.token(j.first + at + c) << (16 * (c & 1));
                     ++n, ++tiles;
                     max_rank = std::max(max_rank, rank);
+                    odd |= odd_rank;
                     if (n == bd::kLoraRecords)
                         if (const hipError_t e = flush(); e != hipSuccess) return e;
                 }
             } else {
-                bd::LoraJob& t = a.job[n];
+                bd::LoraJob& t = a.jobs.job[n];
                 t = bd::LoraJob{};
                 t.w = w;
                 t.hrow = (int32_t)(m * T + j.first);
                 t.tenant = j.tenant;
                 t.count = j.count;
-                t.tile_begin = tiles;
+                a.jobs.tile_begin[n] = tiles;
                 t.first = j.first;
                 t.rank = (uint16_t)rank;
                 t.mat = (uint16_t)m;
                 ++n;
                 tiles += (j.count + columns - 1) / columns;
                 max_rank = std::max(max_rank, rank);
+                odd |= odd_rank;
                 if (n == bd::kLoraRecords)
                     if (const hipError_t e = flush(); e != hipSuccess) return e;
             }
@@ -136,8 +141,8 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
         if (tenant_of_token[t] < 0 || tenant_of_token[t] >= n_tenants) return BD_ERR_TENANT;
     const Batch batch = group(tenant_of_token, T, n_tenants);
     int max_rank = 0;
-    int64_t max_out = 0;
-    for (int m = 0; m < n_mats; ++m) max_out = std::max(max_out, out[m]);
+    int64_t max_out = 0, min_out = out[0];
+    for (int m = 0; m < n_mats; ++m) max_out = std::max(max_out, out[m]), min_out = std::min(min_out, out[m]);
     for (const Job& j : batch.jobs)
         for (int m = 0; m < n_mats; ++m) {
             const int32_t rank = rank_by[(size_t)m * n_tenants + j.tenant];
@@ -210,7 +215,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
                 *rank = rank_by[at];
                 return rank_by[at] > 0;
             },
-            [&](int rank) { return bd::launch_lora_shrink(*s, columns, false, rank, st); });
+            [&](int rank, bool odd) { return bd::launch_lora_shrink(*s, columns, false, rank, odd, st); });
         if (e != hipSuccess) return BD_ERR_DEVICE;
     }
     auto x2 = std::make_unique<bd::LoraExpandArgs>();
@@ -236,7 +241,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
             // without an adapter there is nothing to do where y is y0
             return (out[m] > 0 || (h && h[m])) && (rank_by[at] > 0 || !(y0 && y0[m] == y[m]));
         },
-        [&](int) { return bd::launch_lora_expand(*x2, expand_columns, false, max_out, st); });
+        [&](int, bool odd) { return bd::launch_lora_expand(*x2, expand_columns, false, min_out, max_out, odd, st); });
     return e == hipSuccess ? BD_OK : BD_ERR_DEVICE;
 }
 
@@ -331,7 +336,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         s->ld = (int32_t)ld;
         s->splits = splits;
         s->split_stride = T * ld;
-        if (for_records(*s, batch, T, 1, columns, weights_of(b_by, false), [&](int rank) { return bd::launch_lora_shrink(*s, columns, true, rank, st); }) != hipSuccess)
+        if (for_records(*s, batch, T, 1, columns, weights_of(b_by, false), [&](int rank, bool odd) { return bd::launch_lora_shrink(*s, columns, true, rank, odd, st); }) != hipSuccess)
             return BD_ERR_DEVICE;
     }
     // ---- g (parts added up) and h as operands of the gradients ----
@@ -426,7 +431,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         x2->ld = (int32_t)ld;
         x2->splits = splits;
         x2->split_stride = T * ld;
-        if (for_records(*x2, batch, T, 1, expand_columns, weights_of(a_by, dx0 != dx), [&](int) { return bd::launch_lora_expand(*x2, expand_columns, true, in, st); }) != hipSuccess)
+        if (for_records(*x2, batch, T, 1, expand_columns, weights_of(a_by, dx0 != dx), [&](int, bool odd) { return bd::launch_lora_expand(*x2, expand_columns, true, in, in, odd, st); }) != hipSuccess)
             return BD_ERR_DEVICE;
     }
     if (!accumulate) {   // gradients of adapters that no token used

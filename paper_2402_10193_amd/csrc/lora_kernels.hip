@@ -27,14 +27,19 @@ __device__ __forceinline__ half8 load8(const uint16_t* p) {   // any 2-byte alig
     __builtin_memcpy(&v, p, 16);
     return v;
 }
-__device__ __forceinline__ half8 load8_first(const uint16_t* p, int64_t n) {   // the first n elements (n < 8), zeros behind them
-    half8 v = {};
+// 8 elements one by one, those behind element `last` repeat it: short rows, rows of odd length
+__device__ __forceinline__ half8 load8_each(const uint16_t* p, int64_t last) {
+    half8 v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < n) v[i] = __builtin_bit_cast(_Float16, p[i]);
+    for (int i = 0; i < 8; ++i) v[i] = *(const _Float16*)(p + (i < last ? i : last));
     return v;
 }
-__device__ __forceinline__ half8 load8_upto(const uint16_t* p, int64_t n) { return n >= 8 ? load8(p) : load8_first(p, n); }
+// v with zeros where element i is not in [first, end)
+__device__ __forceinline__ half8 only(half8 v, int first, int end) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i >= first && i < end ? v[i] : (_Float16)0.0f;
+    return v;
+}
 
 // Rows of 8 halves -> columns: element i of out[j] = element j of in[i].  32 byte permutes.
 __device__ __forceinline__ void transpose8(const half8 (&in)[8], half8 (&out)[8]) {
@@ -89,18 +94,40 @@ __device__ __forceinline__ Where find_tile(const Args& a, int t) {
         u = Where{k.w, k.hrow, k.tenant, k.count, k.rank, k.mat, 0, t};
     } else {
         int j = 0;
-        while (j + 1 < a.n_records && a.job[j + 1].tile_begin <= t) ++j;
-        const LoraJob& k = a.job[j];
-        const int skip = (t - k.tile_begin) * 16 * NT;
+#pragma unroll
+        for (int k = 1; k < kLoraRecords; ++k) j += t >= a.jobs.tile_begin[k] ? 1 : 0;
+        const LoraJob& k = a.jobs.job[j];
+        const int skip = (t - a.jobs.tile_begin[j]) * 16 * NT;
         u = Where{k.w, k.hrow + skip, k.tenant, min(k.count - skip, 16 * NT), k.rank, k.mat, k.first + skip, j};
     }
     return u;
 }
 template <int NT, typename Args>
 __device__ __forceinline__ int token_of(const Args& a, const Where& u, int column) {
-    if constexpr (NT == 1) return a.tile[u.record].col[column];
+    if constexpr (NT == 1) {   // a choice among words that came by a scalar load: no vector load of a kernel argument
+        const LoraTile& t = a.tile[u.record];
+        uint32_t w = t.col[0];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) w = (column >> 1) == k ? t.col[k] : w;
+        return (column & 1) ? w >> 16 : w & 0xFFFFu;
+    }
     const int p = u.first + column;
     return a.order ? a.order[p] : p;
+}
+
+// The tokens of N columns, the loads of the order all at once.
+template <int NT, int N, typename Args>
+__device__ __forceinline__ void tokens_of(const Args& a, const Where& u, const int (&column)[N], int (&token)[N]) {
+    if constexpr (NT == 1) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) token[k] = token_of<NT>(a, u, column[k]);
+    } else if (a.order) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) token[k] = a.order[u.first + column[k]];
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) token[k] = u.first + column[k];
+    }
 }
 
 constexpr int kShrinkThreads = kLoraShrinkWaves * kWave;
@@ -129,57 +156,67 @@ struct Stage {
 // h = A x or g = s B^T dy of one tile, 16 RT ranks and one part of the sum.  The wavefronts divide the part among them; each
 // reads x (and A) straight into matrix-core order (a row's 64 bytes per instruction), the eight sums meet in LDS.
 // Ranks and columns beyond the last repeat others or hold anything: rows and columns do not mix, and what they give is not kept.
-template <bool TR, int NT, int RT>
+template <bool TR, int NT, int RT, bool ODD>
 __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraShrinkArgs a) {
     const Where u = find_tile<NT>(a, blockIdx.x);
     const int rt0 = blockIdx.z * RT;
     if (16 * rt0 >= u.rank) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
     const uint16_t* row[NT];
+    int column[NT], token[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int c = 16 * n + m;
-        row[n] = a.src + (int64_t)token_of<NT>(a, u, c < u.count ? c : 0) * a.K + 8 * g;
-    }
+    for (int n = 0; n < NT; ++n) column[n] = 16 * n + m < u.count ? 16 * n + m : 0;
+    tokens_of<NT>(a, u, column, token);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) row[n] = a.src + (int64_t)token[n] * a.K + 8 * g;
     constexpr size_t kSums = sizeof(float4v) * kLoraShrinkWaves * NT * kWave, kStages = TR ? sizeof(Stage<RT>) * kLoraShrinkWaves : 0;
     __shared__ __align__(16) char lds[kSums > kStages ? kSums : kStages];
     Stage<RT>& stage = ((Stage<RT>*)lds)[wave];
     // backward: the lane's 16-byte pieces of 32 rows of B, where rows are whole pieces; else element by element
     const int width = min(16 * RT, u.rank - 16 * rt0);
-    const bool pieces = u.rank % 8 == 0;
+    const bool pieces = !ODD || u.rank % 8 == 0;
     int piece_row[RT], piece_col[RT];
     const uint16_t* wrow[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         if constexpr (TR) {
             const int at = lane + kWave * r, per_row = width / 8;
-            piece_row[r] = pieces ? at / per_row : 32;   // 32: none
+            piece_row[r] = pieces ? at / per_row : 32;   // 32 and more: none
             piece_col[r] = pieces ? 8 * (at % per_row) : 0;
-            wrow[r] = u.w + (int64_t)piece_row[r] * u.rank + 16 * rt0 + piece_col[r];
+            wrow[r] = u.w + 16 * rt0 + piece_col[r];
         } else {
             const int rank = 16 * (rt0 + r) + m < u.rank ? 16 * (rt0 + r) + m : 0;
             wrow[r] = u.w + (int64_t)rank * a.K + 8 * g;
         }
     }
     float4v acc[RT][NT] = {};
+    // Steps of 32 elements.  A last one of fewer (the backward pass's only: K is then `out`) is the last 32 elements, those zero that
+    // an earlier step has had; a K below 32 is read element by element.
     const int64_t steps = (a.K + 31) / 32, parts = (int64_t)a.splits * kLoraShrinkWaves, part = (int64_t)blockIdx.y * kLoraShrinkWaves + wave;
     const int64_t s0 = steps * part / parts, s1 = steps * (part + 1) / parts;
-    const int64_t whole = a.K / 32 < s1 ? a.K / 32 : s1;   // steps of 32 elements; a last one of fewer is the backward pass's only
+    const int64_t whole = a.K / 32 < s1 ? a.K / 32 : s1;
     auto steps_at = [&](auto count, auto ragged, int64_t s) {   // `count` steps: all their loads, then their products
         constexpr int C = decltype(count)::value;
         constexpr bool kRagged = decltype(ragged)::value;
-        const int64_t left = a.K - 32 * s;                  // (ragged: below 32, one step)
+        const int64_t k0 = kRagged ? (!ODD || a.K >= 32 ? a.K - 32 : 0) : 32 * s;
+        const int had = kRagged ? (int)(32 * s - k0) : 0, end = ODD && kRagged && a.K < 32 ? (int)a.K : 32;   // rows that count: had .. end - 1
         half8 xv[C][NT], wv[C][RT];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) xv[c][n] = kRagged ? load8_upto(row[n] + 32 * s, left - 8 * g) : load8(row[n] + 32 * (s + c));
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                if constexpr (TR)
-                    wv[c][r] = piece_row[r] < (kRagged ? (int)left : 32) ? load8(wrow[r] + 32 * (s + c) * u.rank) : half8{};
+            for (int n = 0; n < NT; ++n) {
+                if (ODD && kRagged && a.K < 32)
+                    xv[c][n] = load8_each(row[n] - 8 * g + min(8 * g, end - 1), max(end - 1 - 8 * g, 0));
                 else
-                    wv[c][r] = load8(wrow[r] + 32 * (s + c));
+                    xv[c][n] = load8(row[n] + k0 + 32 * c);
+                if constexpr (kRagged) xv[c][n] = only(xv[c][n], had - 8 * g, end - 8 * g);
+            }
+            if constexpr (!TR) {
+#pragma unroll
+                for (int r = 0; r < RT; ++r) wv[c][r] = load8(wrow[r] + k0 + 32 * c);
+            } else if (pieces) {   // a lane without a piece reads another's: loads without branches
+#pragma unroll
+                for (int r = 0; r < RT; ++r) wv[c][r] = load8(wrow[r] + (k0 + 32 * c + min(piece_row[r], end - 1)) * u.rank);
             }
         }
 #pragma unroll
@@ -188,11 +225,18 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
                 if (pieces) {
 #pragma unroll
                     for (int r = 0; r < RT; ++r)
-                        if (piece_row[r] < 32) *(half8*)&stage.row[piece_row[r]][piece_col[r]] = wv[c][r];
-                } else {
-                    for (int at = lane; at < 32 * width; at += kWave) {
-                        const int k = at / width, rank = at % width;
-                        stage.row[k][rank] = !kRagged || k < left ? *(const _Float16*)(u.w + (32 * (s + c) + k) * u.rank + 16 * rt0 + rank) : (_Float16)0.0f;
+                        if (piece_row[r] < 32) *(half8*)&stage.row[piece_row[r]][piece_col[r]] = piece_row[r] >= had && piece_row[r] < end ? wv[c][r] : half8{};
+                } else if constexpr (ODD) {
+                    _Float16 v[8 * RT];
+#pragma unroll
+                    for (int k = 0; k < 8 * RT; ++k) {
+                        const int at = lane + kWave * k, r = at / (16 * RT), rank = 16 * rt0 + at % (16 * RT);
+                        v[k] = *(const _Float16*)(u.w + (k0 + 32 * c + min(r, end - 1)) * u.rank + min(rank, u.rank - 1));
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8 * RT; ++k) {
+                        const int at = lane + kWave * k, r = at / (16 * RT);
+                        stage.row[r][at % (16 * RT)] = r >= had && r < end ? v[k] : (_Float16)0.0f;
                     }
                 }
                 __builtin_amdgcn_wave_barrier();
@@ -206,11 +250,12 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
             if constexpr (TR) __builtin_amdgcn_wave_barrier();
         }
     };
-    constexpr int kAtOnce = NT * RT == 1 ? 8 : NT + RT <= 5 ? 4 : 2;   // what the registers hold
+    constexpr int kAtOnce = ODD ? 1 : NT * RT == 1 ? 8 : NT + RT <= 5 ? 4 : 2;   // what the registers hold
     int64_t s = s0;
     for (; s + kAtOnce <= whole; s += kAtOnce) steps_at(std::integral_constant<int, kAtOnce>{}, std::false_type{}, s);
     for (; s < whole; ++s) steps_at(std::integral_constant<int, 1>{}, std::false_type{}, s);
-    if (TR && s < s1) steps_at(std::integral_constant<int, 1>{}, std::true_type{}, s);
+    if constexpr (TR)
+        if (s < s1) steps_at(std::integral_constant<int, 1>{}, std::true_type{}, s);
     const float scale = TR ? a.scale[u.tenant] : 1.0f;
     float* const dst = a.h + (int64_t)blockIdx.y * a.split_stride;
     auto* const sum = (float4v(*)[NT][kWave])lds;
@@ -242,7 +287,7 @@ constexpr int kExpandRanks = 128;   // ranks whose hi and lo are in LDS at a tim
 // neighbours of a token's row in its 8 accumulators, and 16 lanes with 256 bytes of the row: one load of y0 and one store for
 // each.  The 32 elements of an MFMA's sum are 16 ranks, hi in lane groups 0 and 1 and lo in 2 and 3, both with the same weights.
 // y0 and the first weights are asked for before h is prepared: three waits for memory become one.
-template <bool TR, int NT>
+template <bool TR, int NT, bool ODD>
 __global__ __launch_bounds__(kExpandThreads) void lora_expand_kernel(const LoraExpandArgs a) {
     constexpr int kTokens = 16 * NT, kPer = kExpandThreads / kTokens;   // threads per token while h is prepared
     constexpr int kPitch = kExpandRanks + 8;
@@ -253,42 +298,59 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_kernel(const LoraE
     if (blockIdx.y > 0 && (int64_t)blockIdx.y * kLoraExpandWaves * kLoraFeatures >= F) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
     const int padded = (u.rank + 15) & ~15;
-    const int64_t f0 = ((int64_t)blockIdx.y * kLoraExpandWaves + wave) * kLoraFeatures, f = f0 + 8 * m;
-    const bool active = f0 < F, inside = f0 + kLoraFeatures <= F;
+    // the wavefront's features, f0 .. f0 + 127; the last one's 128 end with the row and it keeps what is its own; a row below 128 is
+    // read element by element
+    const int64_t f0 = ((int64_t)blockIdx.y * kLoraExpandWaves + wave) * kLoraFeatures, f = min(f0, max(F - kLoraFeatures, (int64_t)0)) + 8 * m;
+    const bool active = f0 < F, vectors = !ODD || F >= kLoraFeatures;
 
     int64_t at[NT][4];   // the rows of y that the lane's results belong to: token 16 n + 4 g + i
     half8 before[NT][4];
+    int column[4 * NT], token[4 * NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int k = 0; k < 4 * NT; ++k) {
+        const int c = 16 * (k >> 2) + 4 * g + (k & 3);
+        column[k] = c < u.count ? c : 0;
+    }
+    tokens_of<NT>(a, u, column, token);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = 16 * n + 4 * g + i;
-            at[n][i] = (int64_t)token_of<NT>(a, u, c < u.count ? c : 0) * F + f;
-        }
+    for (int k = 0; k < 4 * NT; ++k) at[k >> 2][k & 3] = (int64_t)token[k] * F + f;
     const uint16_t* const y0 = active ? a.y0[u.mat] : nullptr;
-    if (y0 && inside) {
+    if (y0 && vectors) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int k = 0; k < 4 * NT; ++k) before[k >> 2][k & 3] = load8(y0 + at[k >> 2][k & 3]);
+    } else if (ODD && y0) {
+        const int64_t back = f < F ? 0 : f - (F - 1);   // a lane behind the row reads its last element
 #pragma unroll
-            for (int i = 0; i < 4; ++i) before[n][i] = load8(y0 + at[n][i]);
+        for (int k = 0; k < 4 * NT; ++k) before[k >> 2][k & 3] = load8_each(y0 + at[k >> 2][k & 3] - back, F - 1 - f + back);
     } else {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) before[n][i] = y0 && f < F ? load8_upto(y0 + at[n][i], F - f) : half8{};
+        for (int k = 0; k < 4 * NT; ++k) before[k >> 2][k & 3] = half8{};
     }
     half8 wv[8];   // forward: the weights of 16 ranks; backward: 8 ranks' rows of A, still to be turned
     auto load_weights = [&](int r) {
         const int rank = r + 8 * (g & 1), left = u.rank - rank;
         if constexpr (TR) {
-            const int64_t col = f <= F - 8 ? f : F - 8;   // (F = in, a multiple of 32)
+            const uint16_t* const w = u.w + (f <= F - 8 ? f : F - 8);   // (F = in, a multiple of 32)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) wv[i] = i < left ? load8(u.w + (int64_t)(rank + i) * F + col) : half8{};
+            for (int i = 0; i < 8; ++i) wv[i] = load8(w + (int64_t)(i < left ? rank + i : u.rank - 1) * F);
+            if (u.rank - r < 16) {   // rows beyond the rank repeat the last one: they do not count
+#pragma unroll
+                for (int i = 0; i < 8; ++i) wv[i] = i < left ? wv[i] : half8{};
+            }
         } else {
+            const uint16_t* w[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int64_t row = f + j < F ? f + j : F - 1;
-                wv[j] = load8_upto(u.w + row * u.rank + rank, left);
+            for (int j = 0; j < 8; ++j) w[j] = u.w + (f + j < F ? f + j : F - 1) * u.rank;
+            if (!ODD || u.rank % 8 == 0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) wv[j] = load8(w[j] + (left > 0 ? rank : r));
+                if (u.rank - r < 16) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) wv[j] = left > 0 ? wv[j] : half8{};
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) wv[j] = only(load8_each(w[j] + (left > 0 ? rank : r), left > 0 ? left - 1 : 0), 0, left);
             }
         }
     };
@@ -298,8 +360,12 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_kernel(const LoraE
     const bool real = c < u.count;
     const float* const src = a.h + (int64_t)(u.hrow + (real ? c : 0)) * a.ld;
     auto sum4 = [&](int r) {
-        float4v v = *(const float4v*)(src + r);
-        for (int s = 1; s < a.splits; ++s) v += *(const float4v*)(src + s * a.split_stride + r);
+        float4v part[kLoraMaxSplits];   // all loads before the first addition
+#pragma unroll
+        for (int s = 0; s < kLoraMaxSplits; ++s) part[s] = s < a.splits ? *(const float4v*)(src + s * a.split_stride + r) : float4v{};
+        float4v v = part[0];
+#pragma unroll
+        for (int s = 1; s < kLoraMaxSplits; ++s) v += part[s];
         return v;
     };
     float top = 0.0f;
@@ -365,12 +431,12 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_kernel(const LoraE
             half8 v;
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = (_Float16)((float)before[n][i][j] + scale * (acc[j][n][i] * up));
-            if (F - f >= 8) {
+            if (f >= f0 && F - f >= 8) {
                 __builtin_memcpy(y + at[n][i], &v, 16);
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (j < F - f) *(_Float16*)(y + at[n][i] + j) = v[j];
+                    if (f + j >= f0 && f + j < F) *(_Float16*)(y + at[n][i] + j) = v[j];
             }
         }
 }
@@ -388,26 +454,41 @@ __global__ __launch_bounds__(kPrepThreads) void lora_prep_kernel(const LoraPrepA
     const int chunk = blockIdx.x + a.chunk_first, t0 = (chunk - job.chunk_begin) * 32, rank_all = job.rank, tiles = (rank_all + 15) / 16;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = lane & 15, q = lane >> 4;
     constexpr int kMine = kLoraMaxRank / 16 / (kPrepThreads / kWave);   // rank tiles of a wavefront
+    // tokens and ranks beyond the last repeat it: loads without branches; what they bring is replaced by zeros
+    int64_t at[8];
+    const float* const src = of_h ? a.h : a.g;
+    {
+        int p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = job.first + min(t0 + 8 * q + i, job.count - 1);
+        if (of_h && a.order) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = a.order[p[i]];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) at[i] = (int64_t)p[i] * (of_h ? a.h_ld : a.ld);
+    }
+    const int splits = of_h ? 1 : a.splits;
     float v[kMine][8];
     float top = 0.0f;
 #pragma unroll
     for (int k = 0; k < kMine; ++k) {
-        const int rt = wave + k * (kPrepThreads / kWave), rank = 16 * rt + n;
+        const int rt = wave + k * (kPrepThreads / kWave), rank = 16 * rt + n, column = min(rank, rank_all - 1);
         if (rt >= tiles) continue;
 #pragma unroll
+        for (int i = 0; i < 8; ++i) v[k][i] = src[at[i] + column];
+        for (int s = 1; s < splits; ++s) {
+            float w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = src[s * a.split_stride + at[i] + column];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] += w[i];
+        }
+#pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int t = t0 + 8 * q + i;
-            v[k][i] = 0.0f;
-            if (t >= job.count || rank >= rank_all) continue;
-            const int p = job.first + t;
-            if (of_h) {
-                v[k][i] = a.h[(int64_t)(a.order ? a.order[p] : p) * a.h_ld + rank];
-            } else {
-                float* const at = a.g + (int64_t)p * a.ld + rank;
-                v[k][i] = at[0];
-                for (int s = 1; s < a.splits; ++s) v[k][i] += at[s * a.split_stride];
-                if (a.splits > 1) at[0] = v[k][i];
-            }
+            const bool real = t0 + 8 * q + i < job.count && rank < rank_all;
+            if (splits > 1 && real) a.g[at[i] + column] = v[k][i];
+            v[k][i] = real ? v[k][i] : 0.0f;
             top = fmaxf(top, finite_abs(v[k][i]));
         }
     }
@@ -446,7 +527,7 @@ constexpr int kGradThreads = kLoraGradWaves * kWave;
 // tokens' rows (256 bytes of a row per instruction) and turns the 8 x 8 block in its registers.  The wavefronts divide the tokens
 // and meet in LDS.  The sums are kept in units of the present 32 tokens' exponent; tokens whose largest value is 2^-64 of the
 // largest so far are below what binary32 would keep of them.
-template <int RT>
+template <int RT, bool ODD>
 __global__ __launch_bounds__(kGradThreads) void lora_grad_kernel(const LoraGradArgs a) {
     const int which = (int)blockIdx.z / a.rank_groups, rt0 = (int)blockIdx.z % a.rank_groups * RT;
     const LoraGradSide& side = a.side[which];
@@ -456,25 +537,29 @@ __global__ __launch_bounds__(kGradThreads) void lora_grad_kernel(const LoraGradA
     const int64_t F = side.F, f0 = (int64_t)blockIdx.x * kLoraFeatures;
     if (!result || 16 * rt0 >= rank_all || f0 >= F) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
-    const int64_t fl = f0 + 8 * m;
+    const int64_t base = min(f0, max(F - kLoraFeatures, (int64_t)0)), fl = base + 8 * m;   // the last 128 features end with the row
     const int steps = (count + 31) / 32, parts = a.token_splits * kLoraGradWaves, part = split * kLoraGradWaves + wave;
     const int s0 = (int)((int64_t)steps * part / parts), s1 = (int)((int64_t)steps * (part + 1) / parts);
-    const bool inside = f0 + kLoraFeatures <= F;
+    const bool vectors = !ODD || F >= kLoraFeatures;
+    const int64_t back = fl < F ? 0 : fl - (F - 1);
     half8 rows[8];
-    auto load_rows = [&](int s) {
-        const int t0 = 32 * s + 8 * g;
-        if (inside && 32 * s + 32 <= count) {
+    auto load_rows = [&](int s) {   // tokens beyond the last repeat it: loads without branches
+        int64_t at[8];
+        int p[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int p = first + t0 + i;
-                rows[i] = load8(side.d + (int64_t)(a.order ? a.order[p] : p) * F + fl);
-            }
+        for (int i = 0; i < 8; ++i) p[i] = first + min(32 * s + 8 * g + i, count - 1);
+        if (a.order) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = a.order[p[i]];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) at[i] = p[i] * F + fl;
+        if (vectors) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rows[i] = load8(side.d + at[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int p = first + t0 + i;
-                rows[i] = t0 + i < count && fl < F ? load8_upto(side.d + (int64_t)(a.order ? a.order[p] : p) * F + fl, F - fl) : half8{};
-            }
+            for (int i = 0; i < 8; ++i) rows[i] = load8_each(side.d + at[i] - back, F - 1 - fl + back);
         }
     };
     float4v acc[8][RT] = {};
@@ -490,6 +575,10 @@ __global__ __launch_bounds__(kGradThreads) void lora_grad_kernel(const LoraGradA
                 hi[r] = op[2 * r * kWave];
                 lo[r] = op[(2 * r + 1) * kWave];
             }
+        if (32 * s + 32 > count) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rows[i] = 32 * s + 8 * g + i < count ? rows[i] : half8{};
+        }
         half8 dv[8];
         transpose8(rows, dv);
         if (s + 1 < s1) load_rows(s + 1);
@@ -533,12 +622,12 @@ __global__ __launch_bounds__(kGradThreads) void lora_grad_kernel(const LoraGradA
             const int at = threadIdx.x + k * kGradThreads;   // of 16 x 128
             const int n = which == 0 ? at / kLoraFeatures : at & 15, f = which == 0 ? at % kLoraFeatures : at >> 4;
             const int row = f >> 3, j = f & 7, rank = 16 * (rt0 + r) + n;
-            if (rank >= rank_all || f0 + f >= F) continue;
+            if (rank >= rank_all || base + f < f0 || base + f >= F) continue;
             float v = 0.0f;
 #pragma unroll
             for (int w = 0; w < kLoraGradWaves; ++w) v += sum[w][j][row & 3][16 * (row >> 2) + n];
             v *= scale;
-            float* const p = out + (which == 0 ? (int64_t)rank * F + f0 + f : (f0 + f) * rank_all + rank);
+            float* const p = out + (which == 0 ? (int64_t)rank * F + base + f : (base + f) * rank_all + rank);
             *p = add ? *p + v : v;
         }
     }
@@ -559,28 +648,30 @@ __global__ __launch_bounds__(256) void lora_reduce_kernel(const LoraReduceArgs a
 static_assert(sizeof(LoraShrinkArgs) <= 4096 && sizeof(LoraExpandArgs) <= 4096 && sizeof(LoraGradArgs) <= 4096 && sizeof(LoraReduceArgs) <= 4096 && sizeof(LoraPrepArgs) <= 4096,
               "kernel arguments");
 
-hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transposed, int max_rank, hipStream_t st) {
+hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transposed, int max_rank, bool odd, hipStream_t st) {
     const int rank_tiles = (max_rank + 15) / 16;
-    if (a.n_tiles < 1 || rank_tiles < 1 || a.splits < 1) return hipErrorInvalidValue;
+    if (a.n_tiles < 1 || rank_tiles < 1 || a.splits < 1 || a.splits > kLoraMaxSplits) return hipErrorInvalidValue;
     auto go = [&](auto kernel, int RT) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)a.splits, (unsigned)((rank_tiles + RT - 1) / RT)), dim3(kShrinkThreads), 0, st, a);
         return hipGetLastError();
     };
-    if (columns == 16) return transposed ? go(lora_shrink_kernel<true, 1, 1>, 1) : go(lora_shrink_kernel<false, 1, 1>, 1);
-    if (rank_tiles == 1) return transposed ? go(lora_shrink_kernel<true, 4, 1>, 1) : go(lora_shrink_kernel<false, 4, 1>, 1);
-    return transposed ? go(lora_shrink_kernel<true, 4, 4>, 4) : go(lora_shrink_kernel<false, 4, 4>, 4);
+    odd |= a.K < 32;
+    if (columns == 16) return !transposed ? go(lora_shrink_kernel<false, 1, 1, false>, 1) : odd ? go(lora_shrink_kernel<true, 1, 1, true>, 1) : go(lora_shrink_kernel<true, 1, 1, false>, 1);
+    if (rank_tiles == 1) return !transposed ? go(lora_shrink_kernel<false, 4, 1, false>, 1) : odd ? go(lora_shrink_kernel<true, 4, 1, true>, 1) : go(lora_shrink_kernel<true, 4, 1, false>, 1);
+    return !transposed ? go(lora_shrink_kernel<false, 4, 4, false>, 4) : odd ? go(lora_shrink_kernel<true, 4, 4, true>, 4) : go(lora_shrink_kernel<true, 4, 4, false>, 4);
 }
 
-hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int64_t max_F, hipStream_t st) {
+hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int64_t min_F, int64_t max_F, bool odd, hipStream_t st) {
     constexpr int64_t per_group = kLoraExpandWaves * kLoraFeatures;
     const int64_t groups = max_F > 0 ? (max_F + per_group - 1) / per_group : 1;   // (F = 0: h alone)
-    if (a.n_tiles < 1 || groups > 65535) return hipErrorInvalidValue;
+    if (a.n_tiles < 1 || groups > 65535 || a.splits > kLoraMaxSplits) return hipErrorInvalidValue;
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)groups), dim3(kExpandThreads), 0, st, a);
         return hipGetLastError();
     };
-    if (columns == 16) return transposed ? go(lora_expand_kernel<true, 1>) : go(lora_expand_kernel<false, 1>);
-    return transposed ? go(lora_expand_kernel<true, 2>) : go(lora_expand_kernel<false, 2>);
+    odd = (odd && !transposed) || min_F < kLoraFeatures;
+    if (columns == 16) return transposed ? (odd ? go(lora_expand_kernel<true, 1, true>) : go(lora_expand_kernel<true, 1, false>)) : odd ? go(lora_expand_kernel<false, 1, true>) : go(lora_expand_kernel<false, 1, false>);
+    return transposed ? (odd ? go(lora_expand_kernel<true, 2, true>) : go(lora_expand_kernel<true, 2, false>)) : odd ? go(lora_expand_kernel<false, 2, true>) : go(lora_expand_kernel<false, 2, false>);
 }
 
 hipError_t launch_lora_prep(const LoraPrepArgs& a, int chunks, int sides, hipStream_t st) {
@@ -599,7 +690,10 @@ hipError_t launch_lora_grad(const LoraGradArgs& a, int max_rank, hipStream_t st)
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)(b.n_jobs * b.token_splits), (unsigned)(2 * b.rank_groups)), dim3(kGradThreads), 0, st, b);
         return hipGetLastError();
     };
-    return RT == 1 ? go(lora_grad_kernel<1>) : RT == 2 ? go(lora_grad_kernel<2>) : go(lora_grad_kernel<4>);
+    // rows below 128 elements (a side that is not wanted has none)
+    const bool odd = (a.side[0].F > 0 && a.side[0].F < kLoraFeatures) || (a.side[1].F > 0 && a.side[1].F < kLoraFeatures);
+    if (odd) return RT == 1 ? go(lora_grad_kernel<1, true>) : RT == 2 ? go(lora_grad_kernel<2, true>) : go(lora_grad_kernel<4, true>);
+    return RT == 1 ? go(lora_grad_kernel<1, false>) : RT == 2 ? go(lora_grad_kernel<2, false>) : go(lora_grad_kernel<4, false>);
 }
 
 hipError_t launch_lora_reduce(const LoraReduceArgs& a, int64_t max_n, hipStream_t st) {
