@@ -17,7 +17,8 @@ constexpr int kLoraMaxMats = 3;
 constexpr int kLoraRecords = 64;        // records of one launch
 constexpr int kLoraMaxSplits = 8;       // parts that the shrink's sum may be cut into
 constexpr int kLoraFeatures = 128;      // output features of one wavefront's step: 8 MFMA rows of 16
-constexpr int kLoraShrinkWaves = 8;
+constexpr int kLoraExpandTokens = 64;   // tokens of a tile where there are many
+constexpr int kLoraShrinkWaves = 4;
 constexpr int kLoraExpandWaves = 4;
 constexpr int kLoraGradWaves = 4;
 
@@ -90,36 +91,41 @@ struct LoraPrepArgs {
 };
 
 // side 0: dA [r][F] = sum over a job's tokens of g[token][r] x[token][f];  side 1: dB [F][r] = scale * sum of dy[token][f] h[token][r]
+constexpr int kLoraGradJobs = 52;
 struct LoraGradJob {
     float* out[2];                      // nullptr: not wanted
-    int64_t part;                       // ranks of the jobs before it in `partial`
-    int32_t tenant, count, first, rank, chunk_begin;
+    int32_t partial;                    // where its parts begin in `partial`, in rows of F
+    int32_t tenant, count, first, rank, chunk_begin, parts;
 };
 struct LoraGradSide {
     const uint16_t* d;                  // [T, F]
     const half8* operand;
     const int32_t* exponent;
     const float* scale;                 // dB: device, by tenant; dA: nullptr (g has it)
-    float* partial;                     // [token_splits][part_stride], used where token_splits > 1
-    int64_t F, part_stride;
+    float* partial;                     // the sums of jobs whose tokens are in several parts: [part][rank * F]
+    int64_t F;
 };
 struct LoraGradArgs {
     const int32_t* order;
     LoraGradSide side[2];
-    int32_t ld, token_splits, n_jobs, accumulate, rank_groups;
-    LoraGradJob job[kLoraRecords - 8];
+    int32_t ld, n_jobs, n_parts, accumulate, rank_groups;
+    int32_t part_begin[kLoraGradJobs];  // first part of every job; behind the last one the largest int
+    LoraGradJob job[kLoraGradJobs];
 };
-constexpr int kLoraGradJobs = kLoraRecords - 8;
-// out (+)= sum over the splits of the partial sums; or zeros (token_splits = 0) for gradients of tenants without a token
+// out (+)= sum over the parts; or zeros (parts = 0) for gradients of tenants without a token
 struct LoraReduceArgs {
-    int32_t token_splits, n_jobs, accumulate;
-    struct { float* out; const float* partial; int64_t part_stride, n; } job[kLoraRecords];
+    int32_t n_jobs, accumulate;
+    struct { float* out; const float* partial; int64_t n; int32_t parts; } job[kLoraRecords];
 };
 
-// `columns`: tokens of a tile (16: records are tiles; else records are jobs, 64 for the shrink, 32 for the expand).  max_rank: the largest rank of the records;
+// workgroups of the shrink for one tile and part of the sum, and how many run on a compute unit at a time
+constexpr int kLoraShrinkAtOnce = 2;
+constexpr int lora_shrink_groups(int rank, int columns) { return (rank + 15) / 16 <= 1 || columns == 16 ? (rank + 15) / 16 : (rank + 63) / 64; }
+
+// `columns`: tokens of a tile (16: records are tiles; else records are jobs, 64).  max_rank: the largest rank of the records;
 // odd: some rank is not a multiple of 8 (B's rows are then no whole 16-byte pieces).
 hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transposed, int max_rank, bool odd, hipStream_t st);
-hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int64_t min_F, int64_t max_F, bool odd, hipStream_t st);
+hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int max_rank, int64_t min_F, int64_t max_F, bool odd, hipStream_t st);
 // prepares `chunks` chunks from a.chunk_first on, of `sides` sides from a.side_first on
 hipError_t launch_lora_prep(const LoraPrepArgs& a, int chunks, int sides, hipStream_t st);
 hipError_t launch_lora_grad(const LoraGradArgs& a, int max_rank, hipStream_t st);

@@ -14,18 +14,30 @@ namespace {
 using bd::misaligned;
 using bd::overlaps;
 
-constexpr int kFewColumns = 16, kShrinkColumns = 64, kExpandColumns = 32;   // tokens of a tile: records are tiles; or jobs, by kernel
+constexpr int kFewColumns = 16, kManyColumns = bd::kLoraExpandTokens;   // tokens of a tile: records are tiles, or jobs
 constexpr int64_t kFewTokens = 512;                  // largest batch whose records are tiles
-constexpr int kGradParts = 16;                       // jobs x parts of the tokens of a gradient, where there is more than one part
+constexpr int kGradParts = 16;                       // parts of jobs whose tokens are in more than one, of all jobs together
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// Parts that the shrink's sum may be cut into: few tokens leave compute units idle.
-int max_splits(int64_t T) { return T <= 2048 ? bd::kLoraMaxSplits : T <= 8192 ? 4 : T <= 16384 ? 2 : 1; }
-int sum_splits(int64_t groups, int64_t K, int64_t T) {
-    const int64_t steps = (K + 31) / 32;   // 8 wavefronts with at least 4 steps each
-    const int64_t most = std::min<int64_t>(max_splits(T), steps / (4 * bd::kLoraShrinkWaves)), want = (256 + groups - 1) / groups;
-    return (int)std::max<int64_t>(1, std::min(most, want));
+int compute_units() {
+    int cus = 256;
+    return bd::device_cu_count(&cus) == hipSuccess && cus > 0 ? cus : 256;
+}
+
+// Parts that the shrink's sum is cut into, where `groups` workgroups take a part each: rounds of what runs at a time, each some 6 us and
+// 0.5 us for every step of its wavefronts (64 tokens; 0.2 of one tile of 16), and 0.3 us more for every part that the next kernel adds up.
+int max_splits(int64_t T) { return T <= 4096 ? bd::kLoraMaxSplits : T <= 16384 ? 4 : T <= 32768 ? 2 : 1; }
+int sum_splits(int64_t groups, int64_t K, int64_t T, bool few) {
+    const int64_t steps = (K + 31) / 32, slots = (int64_t)bd::kLoraShrinkAtOnce * compute_units();
+    int best = 1;
+    double least = 1e30;
+    for (int n = 1; n <= max_splits(T) && (n == 1 || n * bd::kLoraShrinkWaves <= steps); ++n) {
+        const double rounds = (double)((groups * n + slots - 1) / slots), per_wave = (double)((steps + n * bd::kLoraShrinkWaves - 1) / (n * bd::kLoraShrinkWaves));
+        const double us = rounds * (6.0 + (few ? 0.2 : 0.5) * per_wave) + 0.3 * n;
+        if (us < least) least = us, best = n;
+    }
+    return best;
 }
 
 struct Job {
@@ -185,7 +197,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
         return BD_ERR_WORKSPACE;
     // ---- checked: launches from here on ----
     const bool few = T <= kFewTokens;
-    const int columns = few ? kFewColumns : kShrinkColumns, expand_columns = few ? kFewColumns : kExpandColumns;
+    const int columns = few ? kFewColumns : kManyColumns;
     const int32_t* order = nullptr;
     if (!few && !batch.order.empty() && max_rank > 0) {
         if (bd::write_int_table(batch.order, (int32_t*)workspace, st) != hipSuccess) return BD_ERR_DEVICE;
@@ -193,11 +205,11 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
     }
     float* const hw = (float*)((char*)workspace + order_bytes(T));
     const int64_t ld = round_up(max_rank, 16);
-    int64_t tiles = 0;
+    int64_t groups = 0;
     for (const Job& j : batch.jobs)
         for (int m = 0; m < n_mats; ++m)
-            tiles += (int64_t)(j.count + columns - 1) / columns * ((rank_by[(size_t)m * n_tenants + j.tenant] + 15) / 16);
-    const int splits = sum_splits(std::max<int64_t>(tiles, 1), in, T);
+            groups += (int64_t)(j.count + columns - 1) / columns * bd::lora_shrink_groups(rank_by[(size_t)m * n_tenants + j.tenant], columns);
+    const int splits = sum_splits(groups, in, T, few);
     if (max_rank > 0) {
         auto s = std::make_unique<bd::LoraShrinkArgs>();
         s->src = x;
@@ -233,7 +245,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
     x2->splits = splits;
     x2->split_stride = n_mats * T * ld;
     const hipError_t e = for_records(
-        *x2, batch, T, n_mats, expand_columns,
+        *x2, batch, T, n_mats, columns,
         [&](int m, int32_t tenant, const uint16_t** w, int* rank) {
             const size_t at = (size_t)m * n_tenants + tenant;
             *w = b_by[at];
@@ -241,8 +253,32 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
             // without an adapter there is nothing to do where y is y0
             return (out[m] > 0 || (h && h[m])) && (rank_by[at] > 0 || !(y0 && y0[m] == y[m]));
         },
-        [&](int, bool odd) { return bd::launch_lora_expand(*x2, expand_columns, false, min_out, max_out, odd, st); });
+        [&](int rank, bool odd) { return bd::launch_lora_expand(*x2, columns, false, rank, min_out, max_out, odd, st); });
     return e == hipSuccess ? BD_OK : BD_ERR_DEVICE;
+}
+
+// Tokens of a part of the gradients' sums: whole jobs, or jobs cut into parts where that fills the compute units better (the parts
+// must then be added up).  A workgroup of `rank` ranks takes some 7 us and 0.5 us (more than 32 ranks: 0.9) for every 128 tokens; 512 run
+// at a time (256).
+int tokens_of_part(const bd::LoraGradJob* job, int n, int64_t wide, int rank) {
+    int longest = 1;
+    for (int i = 0; i < n; ++i) longest = std::max(longest, (int)job[i].count);
+    const int64_t slots = (int64_t)compute_units() * (rank > 32 ? 1 : 2);
+    int best = longest;
+    double least = 1e30;
+    for (int cut = 1; cut <= kGradParts; ++cut) {
+        const int tokens = (int)round_up((longest + cut - 1) / cut, 128);
+        int64_t parts = 0, partial = 0;
+        for (int i = 0; i < n; ++i) {
+            const int64_t p = (job[i].count + tokens - 1) / tokens;
+            parts += p;
+            if (p > 1) partial += p;
+        }
+        if (partial > kGradParts) break;
+        const double us = (double)((parts * wide + slots - 1) / slots) * (7.0 + (rank > 32 ? 0.9 : 0.5) * (tokens / 128)) + (partial ? 4.0 + (double)partial * rank * wide * 128 * 8 / 3e6 : 0.0);
+        if (us < least) least = us, best = tokens;
+    }
+    return best;
 }
 
 bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_t h_ld, const uint16_t* const* a_by, const uint16_t* const* b_by,
@@ -308,7 +344,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         return BD_ERR_WORKSPACE;
     // ---- checked: launches from here on ----
     const bool few = T <= kFewTokens;
-    const int columns = few ? kFewColumns : kShrinkColumns, expand_columns = few ? kFewColumns : kExpandColumns;
+    const int columns = few ? kFewColumns : kManyColumns;
     const int64_t ld = round_up(max_rank, 16);
     const int32_t* order = nullptr;
     if (work && !batch.order.empty()) {   // (the gradients' sums run over a job's tokens, for few tokens too)
@@ -316,9 +352,9 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         order = (const int32_t*)workspace;
     }
     float* const g = work ? (float*)((char*)workspace + order_bytes(T)) : nullptr;
-    int64_t tiles = 0;
-    for (const Job& j : batch.jobs) tiles += (int64_t)(j.count + columns - 1) / columns * ((rank_by[j.tenant] + 15) / 16);
-    int splits = sum_splits(std::max<int64_t>(tiles, 1), out, T);
+    int64_t groups = 0;
+    for (const Job& j : batch.jobs) groups += (int64_t)(j.count + columns - 1) / columns * bd::lora_shrink_groups(rank_by[j.tenant], columns);
+    int splits = sum_splits(groups, out, T, few);
     auto weights_of = [&](const uint16_t* const* by, bool all) {
         return [=](int, int32_t tenant, const uint16_t** w, int* rank) {
             *rank = rank_by[tenant];
@@ -379,44 +415,50 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         int32_t chunk = 0;
         for (size_t first = 0; first < wanted.size(); first += bd::kLoraGradJobs) {
             const int n = (int)std::min<size_t>(bd::kLoraGradJobs, wanted.size() - first);
-            int64_t part = 0;
-            int most = 0, longest = 0;
+            int most = 0;
             prep->chunk_first = chunk;
             for (int i = 0; i < n; ++i) {
                 const Job& j = wanted[first + (size_t)i];
                 const int rank = rank_by[j.tenant];
                 prep->job[i] = bd::LoraPrepJob{j.first, j.count, rank, chunk};
                 args->job[i] = bd::LoraGradJob{{da_by && in > 0 ? da_by[j.tenant] : nullptr, db_by && out > 0 ? db_by[j.tenant] : nullptr},
-                                               part, j.tenant, j.count, j.first, rank, chunk};
+                                               0, j.tenant, j.count, j.first, rank, chunk, 1};
                 chunk += (j.count + 31) / 32;
-                part += rank;
                 most = std::max(most, rank);
-                longest = std::max(longest, (int)j.count);
             }
             prep->n_jobs = args->n_jobs = n;
             if (bd::launch_lora_prep(*prep, chunk - prep->chunk_first, (any_da ? 1 : 0) + (any_db ? 1 : 0), st) != hipSuccess) return BD_ERR_DEVICE;
-            const int64_t groups = n * ((args->side[0].F + bd::kLoraFeatures - 1) / bd::kLoraFeatures + (args->side[1].F + bd::kLoraFeatures - 1) / bd::kLoraFeatures);
-            if (groups == 0) continue;
-            // few workgroups: the tokens of a job in parts of at least 256
-            args->token_splits = (int)std::max<int64_t>(1, std::min({(1024 + groups - 1) / groups, (int64_t)kGradParts / n, (int64_t)longest / 256}));
-            for (int side = 0; side < 2; ++side) args->side[side].part_stride = part * args->side[side].F;
-            if (bd::launch_lora_grad(*args, most, st) != hipSuccess) return BD_ERR_DEVICE;
-            if (args->token_splits == 1) continue;
-            auto sum = std::make_unique<bd::LoraReduceArgs>();   // (token_splits > 1: 8 jobs at most)
-            sum->token_splits = args->token_splits;
+            const int64_t wide = (args->side[0].F + bd::kLoraFeatures - 1) / bd::kLoraFeatures + (args->side[1].F + bd::kLoraFeatures - 1) / bd::kLoraFeatures;
+            if (wide == 0) continue;
+            const int tokens = tokens_of_part(args->job, n, wide * ((most + 63) / 64), most);
+            auto sum = std::make_unique<bd::LoraReduceArgs>();
             sum->accumulate = args->accumulate;
             int64_t max_n = 0;
-            for (int i = 0; i < n; ++i)
+            int32_t rows = 0;
+            args->n_parts = 0;
+            for (int i = 0; i < bd::kLoraGradJobs; ++i) {
+                if (i >= n) {
+                    args->part_begin[i] = INT32_MAX;
+                    continue;
+                }
+                bd::LoraGradJob& j = args->job[i];
+                args->part_begin[i] = args->n_parts;
+                j.parts = (j.count + tokens - 1) / tokens;
+                args->n_parts += j.parts;
+                if (j.parts == 1) continue;
+                j.partial = rows;
                 for (int side = 0; side < 2; ++side) {
-                    const bd::LoraGradSide& v = args->side[side];
-                    if (!args->job[i].out[side]) continue;
+                    if (!j.out[side]) continue;
                     auto& r = sum->job[sum->n_jobs++];
-                    r.out = args->job[i].out[side];
-                    r.partial = v.partial + args->job[i].part * v.F;
-                    r.part_stride = v.part_stride;
-                    r.n = args->job[i].rank * v.F;
+                    r.out = j.out[side];
+                    r.partial = args->side[side].partial + (int64_t)rows * args->side[side].F;
+                    r.n = j.rank * args->side[side].F;
+                    r.parts = j.parts;
                     max_n = std::max(max_n, r.n);
                 }
+                rows += j.parts * j.rank;
+            }
+            if (bd::launch_lora_grad(*args, most, st) != hipSuccess) return BD_ERR_DEVICE;
             if (sum->n_jobs > 0 && bd::launch_lora_reduce(*sum, max_n, st) != hipSuccess) return BD_ERR_DEVICE;
         }
         if (any_da) splits = 1;   // g is whole
@@ -431,7 +473,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         x2->ld = (int32_t)ld;
         x2->splits = splits;
         x2->split_stride = T * ld;
-        if (for_records(*x2, batch, T, 1, expand_columns, weights_of(a_by, dx0 != dx), [&](int, bool odd) { return bd::launch_lora_expand(*x2, expand_columns, true, in, in, odd, st); }) != hipSuccess)
+        if (for_records(*x2, batch, T, 1, columns, weights_of(a_by, dx0 != dx), [&](int rank, bool odd) { return bd::launch_lora_expand(*x2, columns, true, rank, in, in, odd, st); }) != hipSuccess)
             return BD_ERR_DEVICE;
     }
     if (!accumulate) {   // gradients of adapters that no token used
@@ -439,7 +481,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         int n = 0;
         int64_t max_n = 0;
         auto flush = [&]() {
-            zero->n_jobs = n;   // (token_splits = 0: the sum of nothing)
+            zero->n_jobs = n;   // (no parts: the sum of nothing)
             const bool ok = n == 0 || bd::launch_lora_reduce(*zero, max_n, st) == hipSuccess;
             n = 0;
             max_n = 0;

@@ -16,6 +16,7 @@
 #include <algorithm>
 
 #include "bd_device.h"
+#include "bd_launch.h"
 #include "bd_lora.h"
 
 namespace bd {
@@ -153,8 +154,25 @@ struct Stage {
     }
 };
 
-// h = A x or g = s B^T dy of one tile, 16 RT ranks and one part of the sum.  The wavefronts divide the part among them; each
-// reads x (and A) straight into matrix-core order (a row's 64 bytes per instruction), the eight sums meet in LDS.
+// 16 N rows of 64 bytes: lane 4 r + p has loaded bytes 16 p of row r of each 16 (neighbouring lanes neighbouring bytes; the other way
+// round an instruction takes the address unit four times as long).  Through a piece of LDS of the wavefront's own they come to lane
+// 16 p + r.  The pitch of 80 keeps both accesses free of bank conflicts.
+template <int N>
+struct Turn {
+    char row[16 * N][80];
+
+    __device__ __forceinline__ void operator()(const half8 (&v)[N], half8 (&o)[N], int lane) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) *(half8*)&row[16 * n + (lane >> 2)][16 * (lane & 3)] = v[n];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int n = 0; n < N; ++n) o[n] = *(const half8*)&row[16 * n + (lane & 15)][16 * (lane >> 4)];
+        __builtin_amdgcn_wave_barrier();
+    }
+};
+
+// h = A x or g = s B^T dy of one tile, 16 RT ranks and one part of the sum.  The wavefronts divide the part among them, their
+// sums meet in LDS.  Of one tile of 16 tokens x (and A) is read straight into matrix-core order, which is less to wait for.
 // Ranks and columns beyond the last repeat others or hold anything: rows and columns do not mix, and what they give is not kept.
 template <bool TR, int NT, int RT, bool ODD>
 __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraShrinkArgs a) {
@@ -162,16 +180,20 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
     const int rt0 = blockIdx.z * RT;
     if (16 * rt0 >= u.rank) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
+    constexpr bool kMoved = NT > 1;
+    const int mr = kMoved ? lane >> 2 : m, mp = kMoved ? lane & 3 : g;   // the row and the 16 bytes of 64 that the lane loads
     const uint16_t* row[NT];
     int column[NT], token[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) column[n] = 16 * n + m < u.count ? 16 * n + m : 0;
+    for (int n = 0; n < NT; ++n) column[n] = 16 * n + mr < u.count ? 16 * n + mr : 0;
     tokens_of<NT>(a, u, column, token);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) row[n] = a.src + (int64_t)token[n] * a.K + 8 * g;
-    constexpr size_t kSums = sizeof(float4v) * kLoraShrinkWaves * NT * kWave, kStages = TR ? sizeof(Stage<RT>) * kLoraShrinkWaves : 0;
-    __shared__ __align__(16) char lds[kSums > kStages ? kSums : kStages];
-    Stage<RT>& stage = ((Stage<RT>*)lds)[wave];
+    for (int n = 0; n < NT; ++n) row[n] = a.src + (int64_t)token[n] * a.K + 8 * mp;
+    // a wavefront's piece of LDS takes B, then (A, then) x; at the end all of it takes the sums
+    constexpr size_t kTurn = kMoved ? sizeof(Turn<(NT > RT ? NT : RT)>) : 0, kStage = TR ? sizeof(Stage<RT>) : 0, kMine = kTurn > kStage ? kTurn : kStage;
+    constexpr size_t kSums = sizeof(float4v) * kLoraShrinkWaves * RT * NT * kWave;
+    __shared__ __align__(16) char lds[kSums > kLoraShrinkWaves * kMine ? kSums : kLoraShrinkWaves * kMine];
+    Stage<RT>& stage = *(Stage<RT>*)(lds + wave * kMine);
     // backward: the lane's 16-byte pieces of 32 rows of B, where rows are whole pieces; else element by element
     const int width = min(16 * RT, u.rank - 16 * rt0);
     const bool pieces = !ODD || u.rank % 8 == 0;
@@ -181,115 +203,143 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
     for (int r = 0; r < RT; ++r) {
         if constexpr (TR) {
             const int at = lane + kWave * r, per_row = width / 8;
-            piece_row[r] = pieces ? at / per_row : 32;   // 32 and more: none
+            // (a lane without a piece of its own reads and stores one of the last row's once more: no branches)
+            piece_row[r] = pieces ? min(at / per_row, 31) : 0;
             piece_col[r] = pieces ? 8 * (at % per_row) : 0;
             wrow[r] = u.w + 16 * rt0 + piece_col[r];
         } else {
-            const int rank = 16 * (rt0 + r) + m < u.rank ? 16 * (rt0 + r) + m : 0;
-            wrow[r] = u.w + (int64_t)rank * a.K + 8 * g;
+            const int rank = 16 * (rt0 + r) + mr < u.rank ? 16 * (rt0 + r) + mr : 0;
+            wrow[r] = u.w + (int64_t)rank * a.K + 8 * mp;
         }
     }
+    const float scale = TR ? a.scale[u.tenant] : 1.0f;
     float4v acc[RT][NT] = {};
     // Steps of 32 elements.  A last one of fewer (the backward pass's only: K is then `out`) is the last 32 elements, those zero that
     // an earlier step has had; a K below 32 is read element by element.
-    const int64_t steps = (a.K + 31) / 32, parts = (int64_t)a.splits * kLoraShrinkWaves, part = (int64_t)blockIdx.y * kLoraShrinkWaves + wave;
-    const int64_t s0 = steps * part / parts, s1 = steps * (part + 1) / parts;
-    const int64_t whole = a.K / 32 < s1 ? a.K / 32 : s1;
-    auto steps_at = [&](auto count, auto ragged, int64_t s) {   // `count` steps: all their loads, then their products
-        constexpr int C = decltype(count)::value;
-        constexpr bool kRagged = decltype(ragged)::value;
-        const int64_t k0 = kRagged ? (!ODD || a.K >= 32 ? a.K - 32 : 0) : 32 * s;
-        const int had = kRagged ? (int)(32 * s - k0) : 0, end = ODD && kRagged && a.K < 32 ? (int)a.K : 32;   // rows that count: had .. end - 1
-        half8 xv[C][NT], wv[C][RT];
+    // The wavefronts of a workgroup take neighbouring steps, so that what it reads of a row at a time is a run of 256 bytes.
+    const int64_t parts = (int64_t)a.splits * kLoraShrinkWaves, part = (int64_t)blockIdx.y * kLoraShrinkWaves + wave;
+    const int64_t whole = a.K / 32, mine = part < whole ? (whole - part + parts - 1) / parts : 0;   // steps part, part + parts, ...
+    constexpr int C = ODD ? 1 : NT * RT == 1 ? 4 : NT + RT <= 5 ? 2 : 1;   // steps of one of two buffers: what the registers hold
+    half8 xv[2][C][NT], wv[2][C][RT];
+    auto load = [&](int buffer, int64_t s) {   // (a step beyond the last repeats it)
 #pragma unroll
         for (int c = 0; c < C; ++c) {
+            const int64_t k0 = 32 * (part + parts * min(s + c, mine - 1));
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                if (ODD && kRagged && a.K < 32)
-                    xv[c][n] = load8_each(row[n] - 8 * g + min(8 * g, end - 1), max(end - 1 - 8 * g, 0));
-                else
-                    xv[c][n] = load8(row[n] + k0 + 32 * c);
-                if constexpr (kRagged) xv[c][n] = only(xv[c][n], had - 8 * g, end - 8 * g);
-            }
-            if constexpr (!TR) {
-#pragma unroll
-                for (int r = 0; r < RT; ++r) wv[c][r] = load8(wrow[r] + k0 + 32 * c);
-            } else if (pieces) {   // a lane without a piece reads another's: loads without branches
-#pragma unroll
-                for (int r = 0; r < RT; ++r) wv[c][r] = load8(wrow[r] + (k0 + 32 * c + min(piece_row[r], end - 1)) * u.rank);
-            }
-        }
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            if constexpr (TR) {
-                if (pieces) {
-#pragma unroll
-                    for (int r = 0; r < RT; ++r)
-                        if (piece_row[r] < 32) *(half8*)&stage.row[piece_row[r]][piece_col[r]] = piece_row[r] >= had && piece_row[r] < end ? wv[c][r] : half8{};
-                } else if constexpr (ODD) {
-                    _Float16 v[8 * RT];
-#pragma unroll
-                    for (int k = 0; k < 8 * RT; ++k) {
-                        const int at = lane + kWave * k, r = at / (16 * RT), rank = 16 * rt0 + at % (16 * RT);
-                        v[k] = *(const _Float16*)(u.w + (k0 + 32 * c + min(r, end - 1)) * u.rank + min(rank, u.rank - 1));
-                    }
-#pragma unroll
-                    for (int k = 0; k < 8 * RT; ++k) {
-                        const int at = lane + kWave * k, r = at / (16 * RT);
-                        stage.row[r][at % (16 * RT)] = r >= had && r < end ? v[k] : (_Float16)0.0f;
-                    }
-                }
-                __builtin_amdgcn_wave_barrier();
-            }
+            for (int n = 0; n < NT; ++n) xv[buffer][c][n] = load8(row[n] + k0);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const half8 w = TR ? stage.operand(r, lane) : wv[c][r];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) acc[r][n] = mfma(w, xv[c][n], acc[r][n]);
+                if constexpr (!TR)
+                    wv[buffer][c][r] = load8(wrow[r] + k0);
+                else if (pieces)
+                    wv[buffer][c][r] = load8(wrow[r] + (k0 + piece_row[r]) * u.rank);
             }
-            if constexpr (TR) __builtin_amdgcn_wave_barrier();
         }
     };
-    constexpr int kAtOnce = ODD ? 1 : NT * RT == 1 ? 8 : NT + RT <= 5 ? 4 : 2;   // what the registers hold
-    int64_t s = s0;
-    for (; s + kAtOnce <= whole; s += kAtOnce) steps_at(std::integral_constant<int, kAtOnce>{}, std::false_type{}, s);
-    for (; s < whole; ++s) steps_at(std::integral_constant<int, 1>{}, std::false_type{}, s);
-    if constexpr (TR)
-        if (s < s1) steps_at(std::integral_constant<int, 1>{}, std::true_type{}, s);
-    const float scale = TR ? a.scale[u.tenant] : 1.0f;
-    float* const dst = a.h + (int64_t)blockIdx.y * a.split_stride;
-    auto* const sum = (float4v(*)[NT][kWave])lds;
+    // One step: B goes through LDS, rows outside [had, end) as zeros
+    auto product = [&](const half8 (&x)[NT], const half8 (&w)[RT], int64_t k0, int had, int end) {
+        if constexpr (TR) {
+            if (pieces) {
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        if (16 * (rt0 + r) >= u.rank) continue;   // (of the whole workgroup)
-        if (TR || r > 0) __syncthreads();
+                for (int r = 0; r < RT; ++r)
+                    *(half8*)&stage.row[piece_row[r]][piece_col[r]] = piece_row[r] >= had && piece_row[r] < end ? w[r] : half8{};
+            } else if constexpr (ODD) {
+                _Float16 v[8 * RT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) sum[wave][n][lane] = acc[r][n];
-        __syncthreads();
-        for (int t = threadIdx.x; t < NT * kWave; t += kShrinkThreads) {
-            const int n = t / kWave, l = t & (kWave - 1), c = 16 * n + (l & 15), rank = 16 * (rt0 + r) + 4 * (l >> 4);
-            if (c >= u.count) continue;
-            float4v v = sum[0][n][l];
+                for (int k = 0; k < 8 * RT; ++k) {
+                    const int at = lane + kWave * k, r = at / (16 * RT), rank = 16 * rt0 + at % (16 * RT);
+                    v[k] = *(const _Float16*)(u.w + (k0 + min(r, end - 1)) * u.rank + min(rank, u.rank - 1));
+                }
 #pragma unroll
-            for (int w = 1; w < kLoraShrinkWaves; ++w) v += sum[w][n][l];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = rank + i < u.rank ? v[i] * scale : 0.0f;
-            *(float4v*)(dst + (int64_t)(u.hrow + c) * a.ld + rank) = v;
+                for (int k = 0; k < 8 * RT; ++k) {
+                    const int at = lane + kWave * k, r = at / (16 * RT);
+                    stage.row[r][at % (16 * RT)] = r >= had && r < end ? v[k] : (_Float16)0.0f;
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
         }
+        half8 xo[NT], wo[RT];
+        if constexpr (TR) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) wo[r] = stage.operand(r, lane);
+            __builtin_amdgcn_wave_barrier();
+        } else if constexpr (kMoved) {
+            (*(Turn<RT>*)(lds + wave * kMine))(w, wo, lane);
+        }
+        if constexpr (kMoved) (*(Turn<NT>*)(lds + wave * kMine))(x, xo, lane);
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[r][n] = mfma(TR || kMoved ? wo[r] : w[r], kMoved ? xo[n] : x[n], acc[r][n]);
+    };
+    // Two buffers; loads are never under a condition (past the end they repeat the last step's), or the wait for them would be for all.
+    if (mine > 0) {
+        load(0, 0);
+        int64_t s = 0;
+        for (; s + 2 * C <= mine; s += 2 * C) {
+            load(1, s + C);
+#pragma unroll
+            for (int c = 0; c < C; ++c) product(xv[0][c], wv[0][c], 32 * (part + parts * (s + c)), 0, 32);
+            load(0, s + 2 * C);
+#pragma unroll
+            for (int c = 0; c < C; ++c) product(xv[1][c], wv[1][c], 32 * (part + parts * (s + C + c)), 0, 32);
+        }
+        if (C > 1) load(1, s + C);
+#pragma unroll
+        for (int c = 0; c < 2 * C - 1; ++c)
+            if (s + c < mine) product(xv[c / C][c % C], wv[c / C][c % C], 32 * (part + parts * (s + c)), 0, 32);
+    }
+    if constexpr (TR) {
+        if (a.K % 32 != 0 && whole % parts == part) {   // the last step, of fewer than 32
+            const int64_t k0 = !ODD || a.K >= 32 ? a.K - 32 : 0;
+            const int had = (int)(32 * whole - k0), end = ODD && a.K < 32 ? (int)a.K : 32;
+            half8 x[NT], w[RT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if (ODD && a.K < 32)
+                    x[n] = load8_each(row[n] - 8 * mp + min(8 * mp, end - 1), max(end - 1 - 8 * mp, 0));
+                else
+                    x[n] = load8(row[n] + k0);
+                x[n] = only(x[n], had - 8 * mp, end - 8 * mp);
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+                if (pieces) w[r] = load8(wrow[r] + (k0 + min(piece_row[r], end - 1)) * u.rank);   // (rows beyond `end` are stored as zeros)
+            product(x, w, k0, had, end);
+        }
+    }
+    float* const dst = a.h + (int64_t)blockIdx.y * a.split_stride;
+    auto* const sum = (float4v(*)[RT * NT][kWave])lds;
+    if constexpr (TR || kMoved) __syncthreads();
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sum[wave][r * NT + n][lane] = acc[r][n];
+    __syncthreads();
+#pragma unroll
+    for (int t = wave; t < RT * NT; t += kLoraShrinkWaves) {
+        const int c = 16 * (t % NT) + m, rank = 16 * (rt0 + t / NT) + 4 * g;
+        if (c >= u.count || 16 * (rt0 + t / NT) >= u.rank) continue;
+        float4v v = sum[0][t][lane];
+#pragma unroll
+        for (int w = 1; w < kLoraShrinkWaves; ++w) v += sum[w][t][lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = rank + i < u.rank ? v[i] * scale : 0.0f;
+        *(float4v*)(dst + (int64_t)(u.hrow + c) * a.ld + rank) = v;
     }
 }
 
 constexpr int kExpandThreads = kLoraExpandWaves * kWave;
 constexpr int kExpandRanks = 128;   // ranks whose hi and lo are in LDS at a time
 
-// y = y0 + s B h, or dx = dx0 + A^T g, of one tile by 512 features.  h comes in as `splits` partial sums.  Rows of a result are
+// Few tokens: y = y0 + s B h, or dx = dx0 + A^T g, of one tile of 16 tokens by 512 features.  h comes in as `splits` partial sums.  Rows of a result are
 // tokens, columns features: feature 8 n + j of a wavefront's 128 is column n of its MFMA j, so that a lane ends up with 8
 // neighbours of a token's row in its 8 accumulators, and 16 lanes with 256 bytes of the row: one load of y0 and one store for
 // each.  The 32 elements of an MFMA's sum are 16 ranks, hi in lane groups 0 and 1 and lo in 2 and 3, both with the same weights.
 // y0 and the first weights are asked for before h is prepared: three waits for memory become one.
-template <bool TR, int NT, bool ODD>
-__global__ __launch_bounds__(kExpandThreads) void lora_expand_kernel(const LoraExpandArgs a) {
-    constexpr int kTokens = 16 * NT, kPer = kExpandThreads / kTokens;   // threads per token while h is prepared
+template <bool TR, bool ODD>
+__global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const LoraExpandArgs a) {
+    constexpr int NT = 1, kTokens = 16 * NT, kPer = kExpandThreads / kTokens;   // threads per token while h is prepared
     constexpr int kPitch = kExpandRanks + 8;
     __shared__ __align__(16) _Float16 hi[kTokens][kPitch], lo[kTokens][kPitch];
     __shared__ float unit[kTokens];
@@ -427,10 +477,10 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_kernel(const LoraE
         for (int i = 0; i < 4; ++i) {
             const int col = 16 * n + 4 * g + i;
             if (col >= u.count || f >= F) continue;
-            const float up = unit[col];
+            const float up = unit[col] * scale;
             half8 v;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (_Float16)((float)before[n][i][j] + scale * (acc[j][n][i] * up));
+            for (int j = 0; j < 8; ++j) v[j] = (_Float16)__builtin_fmaf(acc[j][n][i], up, (float)before[n][i][j]);
             if (f >= f0 && F - f >= 8) {
                 __builtin_memcpy(y + at[n][i], &v, 16);
             } else {
@@ -439,6 +489,188 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_kernel(const LoraE
                     if (f + j >= f0 && f + j < F) *(_Float16*)(y + at[n][i] + j) = v[j];
             }
         }
+}
+
+// Many tokens: the same of one tile of 64 tokens, 16 for each wavefront, which take 128 features at a time together, gridDim.y of
+// them in turn.  The weights of 128 features by 16 ranks, 16 bytes of them from each thread, go through one of two buffers in LDS
+// (kPieces: [feature][16 ranks] forward, with 16 bytes more behind 8 features; [16 ranks][128 features] backward, with 16 bytes more
+// behind a row), where every wavefront reads them into matrix-core order without bank conflicts: read from memory in that order,
+// neighbouring lanes would be rows apart and an instruction would take the address unit four times as long.  While a piece is used the
+// next but one is on its way, and the next features' y0.
+constexpr int kPieces = 128 * 32 + 16 * 16;
+template <bool TR, bool ODD>
+__global__ __launch_bounds__(kExpandThreads, ODD ? 2 : 3) void lora_expand_many_kernel(const LoraExpandArgs a) {
+    constexpr int kTokens = kLoraExpandTokens, kPer = kExpandThreads / kTokens;   // threads per token while h is prepared
+    extern __shared__ __align__(16) char lds[];
+    __shared__ float unit[kTokens];
+    const Where u = find_tile<kTokens / 16>(a, blockIdx.x);
+    const int64_t F = a.F[u.mat];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
+    const int padded = (u.rank + 15) & ~15, pitch = padded + 8;
+    char* const pieces = lds;
+    _Float16* const hi = (_Float16*)(lds + 2 * kPieces);
+    _Float16* const lo = hi + kTokens * pitch;
+    const int64_t stride = (int64_t)gridDim.y * kLoraFeatures;
+    // Features f0 .. f0 + 127; a row's last 128 end with it, and of them only those from f0 on are kept.  A row below 128 is read element
+    // by element.
+    int64_t f0 = (int64_t)blockIdx.y * kLoraFeatures;
+    const bool vectors = !ODD || F >= kLoraFeatures;
+    auto begin_of = [&](int64_t first) { return min(first, max(F - kLoraFeatures, (int64_t)0)); };
+
+    int64_t row[4];   // the rows of y that the lane's results belong to: token 16 wave + 4 g + i
+    {
+        int column[4], token[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = 16 * wave + 4 * g + i;
+            column[i] = c < u.count ? c : 0;
+        }
+        tokens_of<kTokens / 16>(a, u, column, token);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) row[i] = (int64_t)token[i] * F + 8 * m;
+    }
+    const uint16_t* const y0 = a.y0[u.mat];
+    half8 before[4];
+    auto load_y0 = [&](half8 (&to)[4], int64_t f) {
+        if (y0 && vectors) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) to[i] = load8(y0 + row[i] + f);
+        } else if (ODD && y0) {
+            const int64_t at = 8 * m < F ? 0 : F - 1 - 8 * m;   // a lane behind the row reads its last element
+#pragma unroll
+            for (int i = 0; i < 4; ++i) to[i] = load8_each(y0 + row[i] + at, max(F - 1 - 8 * m, (int64_t)0));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) to[i] = half8{};
+        }
+    };
+    // the thread's 16 bytes of the weights
+    const int piece_row = TR ? (int)threadIdx.x >> 4 : (int)threadIdx.x >> 1, piece_col = TR ? 8 * ((int)threadIdx.x & 15) : 8 * ((int)threadIdx.x & 1);
+    char* const piece_at = pieces + (TR ? piece_row * 272 + piece_col * 2 : piece_row * 32 + piece_col * 2 + (piece_row >> 3) * 16);
+    half8 piece;
+    auto load_piece = [&](int64_t f, int r) {
+        if constexpr (TR) {   // (F = in, a multiple of 32)
+            piece = load8(u.w + (int64_t)min(r + piece_row, u.rank - 1) * F + min(f + piece_col, F - 8));
+            piece = r + piece_row < u.rank ? piece : half8{};
+        } else {
+            const uint16_t* const w = u.w + min(f + piece_row, F - 1) * u.rank;
+            const int left = u.rank - r - piece_col;
+            if (!ODD || u.rank % 8 == 0)
+                piece = load8(w + (left > 0 ? r + piece_col : r));
+            else
+                piece = load8_each(w + (left > 0 ? r + piece_col : r), left > 0 ? left - 1 : 0);
+            piece = ODD ? only(piece, 0, left) : left > 0 ? piece : half8{};
+        }
+    };
+    // the pieces come in the order of their use: 16 ranks after 16 ranks, then the next features; past the end the last once more
+    int64_t piece_f0 = f0;
+    int piece_r = 0;
+    auto next_piece = [&] {
+        load_piece(begin_of(piece_f0), piece_r);
+        if (piece_r + 16 < padded) {
+            piece_r += 16;
+        } else if (piece_f0 + stride < F) {
+            piece_r = 0;
+            piece_f0 += stride;
+        }
+    };
+    const bool work = f0 < F;   // (not for a matrix without outputs, whose h alone is asked for)
+    if (work) {
+        load_y0(before, begin_of(f0));
+        if (padded > 0) next_piece();
+    }
+
+    // h of the tile's tokens: the parts added up, the exponent, hi and lo into LDS
+    const int c = threadIdx.x / kPer, sub = threadIdx.x % kPer;
+    const bool real = c < u.count;
+    const float* const src = a.h + (int64_t)(u.hrow + (real ? c : 0)) * a.ld;
+    auto sum4 = [&](int r) {
+        float4v v = *(const float4v*)(src + r);
+        for (int s = 1; s < a.splits; ++s) v += *(const float4v*)(src + s * a.split_stride + r);
+        return v;
+    };
+    float* const kept = !TR && a.h_out[u.mat] && blockIdx.y == 0 && real ? a.h_out[u.mat] + (int64_t)token_of<kTokens / 16>(a, u, c) * a.h_ld : nullptr;
+    float top = 0.0f;
+    float4v first = {};   // of the thread's first four ranks: all there are of 16
+    for (int r = 4 * sub; r < padded; r += 4 * kPer) {
+        const float4v v = sum4(r);
+        if (r == 4 * sub) first = v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            top = fmaxf(top, finite_abs(v[i]));
+            if (kept && r + i < u.rank) kept[r + i] = v[i];
+        }
+    }
+#pragma unroll
+    for (int d = kPer / 2; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
+    const int e = group_exponent(top);
+    if (sub == 0) unit[c] = power_of_two(e) * (TR || u.rank == 0 ? 1.0f : a.scale[u.mat][u.tenant]);
+    const float down = power_of_two(-e);
+    for (int r = 4 * sub; r < padded; r += 4 * kPer) {
+        const float4v v = r == 4 * sub ? first : sum4(r);
+        half4 h, l;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            _Float16 p, q;
+            split_half(v[i], down, &p, &q);
+            h[i] = real ? p : (_Float16)0.0f;
+            l[i] = real ? q : (_Float16)0.0f;
+        }
+        *(half4*)(hi + c * pitch + r) = h;
+        *(half4*)(lo + c * pitch + r) = l;
+    }
+    if (!work) return;   // (of the whole workgroup)
+    if (padded > 0) {
+        *(half8*)piece_at = piece;
+        next_piece();
+    }
+    __syncthreads();
+
+    uint16_t* const y = a.y[u.mat];
+    const _Float16* const mine = (g < 2 ? hi : lo) + (16 * wave + m) * pitch + 8 * (g & 1);
+    float up[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) up[i] = unit[16 * wave + 4 * g + i];
+    int buffer = 0;
+    for (; f0 < F; f0 += stride) {
+        const int64_t f = begin_of(f0), fl = f + 8 * m;
+        float4v acc[8] = {};
+        for (int r = 0; r < padded; r += 16) {
+            *(half8*)(piece_at + (buffer ^ 1) * kPieces) = piece;   // of the next ranks or features
+            next_piece();
+            const char* const at = pieces + buffer * kPieces + (TR ? 8 * (g & 1) * 272 + m * 16 : m * (8 * 32 + 16) + (g & 1) * 16);
+            half8 wv[8], cols[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) wv[j] = *(const half8*)(at + j * (TR ? 272 : 32));
+            if constexpr (TR) {
+                transpose8(wv, cols);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) cols[j] = wv[j];
+            }
+            const half8 hv = *(const half8*)(mine + r);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] = mfma(hv, cols[j], acc[j]);
+            buffer ^= 1;
+            __syncthreads();
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            half8 v;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = (_Float16)__builtin_fmaf(acc[j][i], up[i], (float)before[i][j]);
+            if (16 * wave + 4 * g + i < u.count) {
+                if (fl >= f0 && F - fl >= 8) {
+                    __builtin_memcpy(y + row[i] + f, &v, 16);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (fl + j >= f0 && fl + j < F) *(_Float16*)(y + row[i] + f + j) = v[j];
+                }
+            }
+        }
+        load_y0(before, begin_of(min(f0 + stride, F - 1)));   // (past the end: the last features' once more)
+    }
 }
 
 constexpr int kPrepThreads = 256;
@@ -531,61 +763,77 @@ template <int RT, bool ODD>
 __global__ __launch_bounds__(kGradThreads) void lora_grad_kernel(const LoraGradArgs a) {
     const int which = (int)blockIdx.z / a.rank_groups, rt0 = (int)blockIdx.z % a.rank_groups * RT;
     const LoraGradSide& side = a.side[which];
-    const LoraGradJob& job = a.job[blockIdx.y / a.token_splits];
-    const int split = blockIdx.y % a.token_splits, rank_all = job.rank, count = job.count, first = job.first;
+    int which_job = 0;
+#pragma unroll
+    for (int k = 1; k < kLoraGradJobs; ++k) which_job += (int)blockIdx.y >= a.part_begin[k] ? 1 : 0;
+    const LoraGradJob& job = a.job[which_job];
+    const int token_parts = job.parts, split = blockIdx.y - a.part_begin[which_job], rank_all = job.rank, count = job.count, first = job.first;
     float* const result = job.out[which];
     const int64_t F = side.F, f0 = (int64_t)blockIdx.x * kLoraFeatures;
     if (!result || 16 * rt0 >= rank_all || f0 >= F) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
     const int64_t base = min(f0, max(F - kLoraFeatures, (int64_t)0)), fl = base + 8 * m;   // the last 128 features end with the row
-    const int steps = (count + 31) / 32, parts = a.token_splits * kLoraGradWaves, part = split * kLoraGradWaves + wave;
+    const int steps = (count + 31) / 32, parts = token_parts * kLoraGradWaves, part = split * kLoraGradWaves + wave;
     const int s0 = (int)((int64_t)steps * part / parts), s1 = (int)((int64_t)steps * (part + 1) / parts);
     const bool vectors = !ODD || F >= kLoraFeatures;
     const int64_t back = fl < F ? 0 : fl - (F - 1);
-    half8 rows[8];
-    auto load_rows = [&](int s) {   // tokens beyond the last repeat it: loads without branches
-        int64_t at[8];
+    // Of steps s, s + 1: rows are asked for two steps ahead, the prepared operand one.  Loads are never under a condition (past the end
+    // they repeat the last step's), or the wait for them would be for all.
+    half8 rows[2][8], op[2][2 * RT];
+    int exponent[2] = {};
+    typedef const __attribute__((address_space(4))) int32_t* scalar_ints;   // read by scalar loads, which vector loads need not wait for
+    auto load_rows = [&](int buffer, int step) {   // tokens beyond the last repeat the step's first
+        const int s = min(step, s1 - 1);
         int p[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = first + min(32 * s + 8 * g + i, count - 1);
         if (a.order) {
+            const scalar_ints ids = (scalar_ints)(a.order + first + 32 * s);
+            int id[32];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = a.order[p[i]];
-        }
+            for (int i = 0; i < 32; ++i) id[i] = 32 * s + i < count ? ids[i] : ids[0];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) at[i] = p[i] * F + fl;
-        if (vectors) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rows[i] = load8(side.d + at[i]);
+            for (int i = 0; i < 8; ++i) p[i] = g == 0 ? id[i] : g == 1 ? id[8 + i] : g == 2 ? id[16 + i] : id[24 + i];
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) rows[i] = load8_each(side.d + at[i] - back, F - 1 - fl + back);
+            for (int i = 0; i < 8; ++i) p[i] = first + (32 * s + 8 * g + i < count ? 32 * s + 8 * g + i : 32 * s);
+        }
+        if (vectors) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rows[buffer][i] = load8(side.d + p[i] * F + fl);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rows[buffer][i] = load8_each(side.d + p[i] * F + fl - back, F - 1 - fl + back);
+        }
+    };
+    auto load_operand = [&](int buffer, int step) {
+        const int chunk = job.chunk_begin + min(step, s1 - 1);
+        exponent[buffer] = ((scalar_ints)side.exponent)[chunk];
+        const half8* const p = side.operand + ((int64_t)chunk * (a.ld / 16) + rt0) * 2 * kWave + lane;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {   // (rank tiles beyond the job's repeat its last)
+            const int t = min(r, (rank_all - 1) / 16 - rt0);
+            op[buffer][2 * r] = p[2 * t * kWave];
+            op[buffer][2 * r + 1] = p[(2 * t + 1) * kWave];
         }
     };
     float4v acc[8][RT] = {};
     int e = -200, largest = -200;   // none yet
-    if (s0 < s1) load_rows(s0);
-    for (int s = s0; s < s1; ++s) {
-        const int chunk = job.chunk_begin + s, now = side.exponent[chunk];
-        const half8* const op = side.operand + ((int64_t)chunk * (a.ld / 16) + rt0) * 2 * kWave + lane;
-        half8 hi[RT], lo[RT];
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-            if (16 * (rt0 + r) < rank_all) {
-                hi[r] = op[2 * r * kWave];
-                lo[r] = op[(2 * r + 1) * kWave];
-            }
+    auto product = [&](auto which_buffer, int s) {
+        constexpr int b = decltype(which_buffer)::value;
+        load_operand(1 - b, s + 1);
+        const int now = exponent[b];
         if (32 * s + 32 > count) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) rows[i] = 32 * s + 8 * g + i < count ? rows[i] : half8{};
+            for (int i = 0; i < 8; ++i) rows[b][i] = 32 * s + 8 * g + i < count ? rows[b][i] : half8{};
         }
         half8 dv[8];
-        transpose8(rows, dv);
-        if (s + 1 < s1) load_rows(s + 1);
-        if (now < largest - 64) continue;
-        largest = max(largest, now);
-        if (now != e) {
-            if (e > -200) {
+        transpose8(rows[b], dv);
+        load_rows(b, s + 2);
+        if (now < largest - 64) {   // too small to count
+#pragma unroll
+            for (int j = 0; j < 8; ++j) dv[j] = half8{};
+        } else {
+            largest = max(largest, now);
+            if (now != e && e > -200) {
                 const float f = e - now < -126 ? 0.0f : power_of_two(e - now);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -595,19 +843,26 @@ __global__ __launch_bounds__(kGradThreads) void lora_grad_kernel(const LoraGradA
             e = now;
         }
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-            if (16 * (rt0 + r) < rank_all) {
+        for (int r = 0; r < 2 * RT; ++r)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j][r] = mfma(dv[j], hi[r], acc[j][r]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j][r] = mfma(dv[j], lo[r], acc[j][r]);
-            }
+            for (int j = 0; j < 8; ++j) acc[j][r / 2] = mfma(dv[j], op[b][r], acc[j][r / 2]);
+    };
+    if (s0 < s1) {
+        load_operand(0, s0);
+        load_rows(0, s0);
+        load_rows(1, s0 + 1);
+        int s = s0;
+        for (; s + 2 <= s1; s += 2) {
+            product(std::integral_constant<int, 0>{}, s);
+            product(std::integral_constant<int, 1>{}, s + 1);
+        }
+        if (s < s1) product(std::integral_constant<int, 0>{}, s);
     }
     const float up = e > -200 ? power_of_two(e) : 0.0f;
     __shared__ float sum[kLoraGradWaves][8][4][kWave];   // [wave][j][i][lane (n, q)] = feature 8 (4 q + i) + j, rank n
     const float scale = side.scale ? side.scale[job.tenant] : 1.0f;
-    float* const out = a.token_splits > 1 ? side.partial + split * side.part_stride + job.part * F : result;
-    const bool add = a.accumulate && a.token_splits == 1;
+    float* const out = token_parts > 1 ? side.partial + (job.partial + (int64_t)split * rank_all) * F : result;
+    const bool add = a.accumulate && token_parts == 1;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         if (16 * (rt0 + r) >= rank_all) continue;   // (of the whole workgroup)
@@ -638,7 +893,7 @@ __global__ __launch_bounds__(256) void lora_reduce_kernel(const LoraReduceArgs a
     const auto& job = a.job[blockIdx.y];
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < job.n; i += (int64_t)gridDim.x * 256) {
         float v = 0.0f;
-        for (int s = 0; s < a.token_splits; ++s) v += job.partial[s * job.part_stride + i];
+        for (int s = 0; s < job.parts; ++s) v += job.partial[s * job.n + i];
         job.out[i] = a.accumulate ? job.out[i] + v : v;
     }
 }
@@ -657,21 +912,37 @@ hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transpo
     };
     odd |= a.K < 32;
     if (columns == 16) return !transposed ? go(lora_shrink_kernel<false, 1, 1, false>, 1) : odd ? go(lora_shrink_kernel<true, 1, 1, true>, 1) : go(lora_shrink_kernel<true, 1, 1, false>, 1);
-    if (rank_tiles == 1) return !transposed ? go(lora_shrink_kernel<false, 4, 1, false>, 1) : odd ? go(lora_shrink_kernel<true, 4, 1, true>, 1) : go(lora_shrink_kernel<true, 4, 1, false>, 1);
-    return !transposed ? go(lora_shrink_kernel<false, 4, 4, false>, 4) : odd ? go(lora_shrink_kernel<true, 4, 4, true>, 4) : go(lora_shrink_kernel<true, 4, 4, false>, 4);
+    if (transposed && odd) return go(lora_shrink_kernel<true, 4, 1, true>, 1);
+    if (rank_tiles == 1) return transposed ? go(lora_shrink_kernel<true, 4, 1, false>, 1) : go(lora_shrink_kernel<false, 4, 1, false>, 1);
+    return transposed ? go(lora_shrink_kernel<true, 4, 4, false>, 4) : go(lora_shrink_kernel<false, 4, 4, false>, 4);
 }
 
-hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int64_t min_F, int64_t max_F, bool odd, hipStream_t st) {
-    constexpr int64_t per_group = kLoraExpandWaves * kLoraFeatures;
-    const int64_t groups = max_F > 0 ? (max_F + per_group - 1) / per_group : 1;   // (F = 0: h alone)
-    if (a.n_tiles < 1 || groups > 65535 || a.splits > kLoraMaxSplits) return hipErrorInvalidValue;
-    auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)groups), dim3(kExpandThreads), 0, st, a);
+hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int max_rank, int64_t min_F, int64_t max_F, bool odd, hipStream_t st) {
+    if (a.n_tiles < 1 || max_rank > kLoraMaxRank || a.splits > kLoraMaxSplits) return hipErrorInvalidValue;
+    odd = (odd && !transposed) || min_F < kLoraFeatures;
+    const int64_t wide = std::max<int64_t>(1, (max_F + kLoraFeatures - 1) / kLoraFeatures);   // (F = 0: h alone)
+    if (columns == 16) {
+        const int64_t groups = (wide + kLoraExpandWaves - 1) / kLoraExpandWaves;
+        if (groups > 65535) return hipErrorInvalidValue;
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)groups), dim3(kExpandThreads), 0, st, a);
+            return hipGetLastError();
+        };
+        return transposed ? (odd ? go(lora_expand_few_kernel<true, true>) : go(lora_expand_few_kernel<true, false>)) : odd ? go(lora_expand_few_kernel<false, true>) : go(lora_expand_few_kernel<false, false>);
+    }
+    int cus = 256;
+    if (const hipError_t e = device_cu_count(&cus); e != hipSuccess) return e;
+    // as many workgroups as run at a time (forward 4 to a compute unit, backward 3), each taking several turns
+    const int64_t turns = std::max<int64_t>(1, std::min<int64_t>(wide, (int64_t)(transposed ? 3 : 4) * cus / a.n_tiles));
+    const unsigned lds = (unsigned)(2 * kPieces + 2 * kLoraExpandTokens * (((max_rank + 15) & ~15) + 8) * 2);
+    static PerDeviceOnce once[4];
+    auto go = [&](auto kernel, int which) {
+        const hipError_t e = once[which].run([&] { return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kPieces + 2 * kLoraExpandTokens * (kLoraMaxRank + 8) * 2); });
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)turns), dim3(kExpandThreads), lds, st, a);
         return hipGetLastError();
     };
-    odd = (odd && !transposed) || min_F < kLoraFeatures;
-    if (columns == 16) return transposed ? (odd ? go(lora_expand_kernel<true, 1, true>) : go(lora_expand_kernel<true, 1, false>)) : odd ? go(lora_expand_kernel<false, 1, true>) : go(lora_expand_kernel<false, 1, false>);
-    return transposed ? (odd ? go(lora_expand_kernel<true, 2, true>) : go(lora_expand_kernel<true, 2, false>)) : odd ? go(lora_expand_kernel<false, 2, true>) : go(lora_expand_kernel<false, 2, false>);
+    return transposed ? (odd ? go(lora_expand_many_kernel<true, true>, 0) : go(lora_expand_many_kernel<true, false>, 1)) : odd ? go(lora_expand_many_kernel<false, true>, 2) : go(lora_expand_many_kernel<false, false>, 3);
 }
 
 hipError_t launch_lora_prep(const LoraPrepArgs& a, int chunks, int sides, hipStream_t st) {
@@ -683,11 +954,11 @@ hipError_t launch_lora_prep(const LoraPrepArgs& a, int chunks, int sides, hipStr
 hipError_t launch_lora_grad(const LoraGradArgs& a, int max_rank, hipStream_t st) {
     const int rank_tiles = (max_rank + 15) / 16, RT = rank_tiles >= 3 ? 4 : rank_tiles;
     const int64_t F = std::max(a.side[0].F, a.side[1].F), groups = (F + kLoraFeatures - 1) / kLoraFeatures;
-    if (a.n_jobs < 1 || rank_tiles < 1 || groups < 1 || a.token_splits < 1) return hipErrorInvalidValue;
+    if (a.n_jobs < 1 || rank_tiles < 1 || groups < 1 || a.n_parts < 1) return hipErrorInvalidValue;
     LoraGradArgs b = a;
     b.rank_groups = (rank_tiles + RT - 1) / RT;
     auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)(b.n_jobs * b.token_splits), (unsigned)(2 * b.rank_groups)), dim3(kGradThreads), 0, st, b);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)b.n_parts, (unsigned)(2 * b.rank_groups)), dim3(kGradThreads), 0, st, b);
         return hipGetLastError();
     };
     // rows below 128 elements (a side that is not wanted has none)
