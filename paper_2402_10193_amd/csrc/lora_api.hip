@@ -16,7 +16,7 @@ using bd::overlaps;
 
 constexpr int kFewColumns = 16, kManyColumns = bd::kLoraExpandTokens;   // tokens of a tile: records are tiles, or jobs
 constexpr int64_t kFewTokens = 512;                  // largest batch whose records are tiles
-constexpr int kGradParts = 16;                       // parts of jobs whose tokens are in more than one, of all jobs together
+constexpr int kGradParts = 32;                       // parts of jobs whose tokens are in more than one, of all jobs together
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
@@ -131,8 +131,9 @@ size_t h_bytes(int64_t T, int32_t n_mats, int32_t max_rank) {
 int64_t most_chunks(int64_t T, int32_t n_tenants) { return T / 32 + std::min<int64_t>(T, n_tenants); }
 size_t operand_bytes(int64_t chunks, int32_t max_rank) { return (size_t)(chunks * (round_up(max_rank, 16) / 16) * 2 * 64 * 16); }
 size_t exponent_bytes(int64_t chunks) { return (size_t)round_up(chunks * 4, 256); }
-size_t grad_part_bytes(int64_t out, int64_t in, int32_t max_rank) {
-    return (size_t)round_up((int64_t)kGradParts * round_up(max_rank, 16) * (in + out) * 4, 256);
+int64_t most_parts(int64_t T) { return std::min<int64_t>(kGradParts, T / 32); }
+size_t grad_part_bytes(int64_t T, int64_t out, int64_t in, int32_t max_rank) {
+    return (size_t)round_up(most_parts(T) * round_up(max_rank, 16) * (in + out) * 4, 256);
 }
 
 bool sizes_ok(int64_t T, int64_t out, int64_t in, int32_t n_tenants) {
@@ -257,28 +258,30 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
     return e == hipSuccess ? BD_OK : BD_ERR_DEVICE;
 }
 
-// Tokens of a part of the gradients' sums: whole jobs, or jobs cut into parts where that fills the compute units better (the parts
-// must then be added up).  A workgroup of `rank` ranks takes some 7 us and 0.5 us (more than 32 ranks: 0.9) for every 128 tokens; 512 run
-// at a time (256).
-int tokens_of_part(const bd::LoraGradJob* job, int n, int64_t wide, int rank) {
+// Parts of every job's tokens in the gradients' sums: one, or more where that fills the compute units better (the parts must then be
+// added up).  A workgroup of RW wavefronts to a tile takes some 5 us and 0.35 us for every tile of 32 tokens that each of its 4 / RW groups
+// takes; 3 or 4 run on a compute unit at a time.
+void cut_into_parts(bd::LoraGradJob* job, int n, int64_t wide, int rank, int64_t most) {
     int longest = 1;
     for (int i = 0; i < n; ++i) longest = std::max(longest, (int)job[i].count);
-    const int64_t slots = (int64_t)compute_units() * (rank > 32 ? 1 : 2);
-    int best = longest;
+    const int RW = bd::lora_grad_rank_waves(rank), TW = bd::kLoraGradWaves / RW;
+    const int64_t slots = (int64_t)compute_units() * (RW == 1 ? 3 : 4);
+    int best = std::min(longest, bd::kLoraPartTokens);
     double least = 1e30;
     for (int cut = 1; cut <= kGradParts; ++cut) {
-        const int tokens = (int)round_up((longest + cut - 1) / cut, 128);
+        const int tokens = std::min((int)round_up((longest + cut - 1) / cut, 32), bd::kLoraPartTokens);
         int64_t parts = 0, partial = 0;
         for (int i = 0; i < n; ++i) {
             const int64_t p = (job[i].count + tokens - 1) / tokens;
             parts += p;
             if (p > 1) partial += p;
         }
-        if (partial > kGradParts) break;
-        const double us = (double)((parts * wide + slots - 1) / slots) * (7.0 + (rank > 32 ? 0.9 : 0.5) * (tokens / 128)) + (partial ? 4.0 + (double)partial * rank * wide * 128 * 8 / 3e6 : 0.0);
+        if (partial > most) continue;
+        const int64_t rounds = (parts * wide + slots - 1) / slots;
+        const double us = (double)rounds * (5.0 + 0.35 * (double)((tokens + 32 * TW - 1) / (32 * TW))) + (partial ? 4.0 + (double)partial * rank * wide * 128 * 8 / 3e6 : 0.0);
         if (us < least) least = us, best = tokens;
     }
-    return best;
+    for (int i = 0; i < n; ++i) job[i].parts = (job[i].count + best - 1) / best;
 }
 
 bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_t h_ld, const uint16_t* const* a_by, const uint16_t* const* b_by,
@@ -401,7 +404,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
             v.exponent = exponent[side];
             v.scale = side ? scale : nullptr;
             v.F = side ? (any_db ? out : 0) : (any_da ? in : 0);
-            v.partial = partial + (side ? (int64_t)kGradParts * ld * in : 0);
+            v.partial = partial + (side ? most_parts(T) * ld * in : 0);
         }
         prep->split_stride = T * ld;
         prep->ld = args->ld = (int32_t)ld;
@@ -430,7 +433,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
             if (bd::launch_lora_prep(*prep, chunk - prep->chunk_first, (any_da ? 1 : 0) + (any_db ? 1 : 0), st) != hipSuccess) return BD_ERR_DEVICE;
             const int64_t wide = (args->side[0].F + bd::kLoraFeatures - 1) / bd::kLoraFeatures + (args->side[1].F + bd::kLoraFeatures - 1) / bd::kLoraFeatures;
             if (wide == 0) continue;
-            const int tokens = tokens_of_part(args->job, n, wide * ((most + 63) / 64), most);
+            cut_into_parts(args->job, n, wide * ((most + 63) / 64), most, most_parts(T));
             auto sum = std::make_unique<bd::LoraReduceArgs>();
             sum->accumulate = args->accumulate;
             int64_t max_n = 0;
@@ -443,7 +446,6 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
                 }
                 bd::LoraGradJob& j = args->job[i];
                 args->part_begin[i] = args->n_parts;
-                j.parts = (j.count + tokens - 1) / tokens;
                 args->n_parts += j.parts;
                 if (j.parts == 1) continue;
                 j.partial = rows;
@@ -516,7 +518,7 @@ size_t bd_lora_workspace_bytes(int64_t T, int32_t n_mats, int32_t max_rank) {
 size_t bd_lora_backward_workspace_bytes(int64_t T, int64_t out, int64_t in, int32_t n_tenants, int32_t max_rank) {
     if (T < 1 || !sizes_ok(T, out, in, n_tenants) || n_tenants < 1 || max_rank < 1 || max_rank > bd::kLoraMaxRank) return 0;
     const int64_t chunks = most_chunks(T, n_tenants);
-    return order_bytes(T) + h_bytes(T, 1, max_rank) + 2 * (operand_bytes(chunks, max_rank) + exponent_bytes(chunks)) + grad_part_bytes(out, in, max_rank);
+    return order_bytes(T) + h_bytes(T, 1, max_rank) + 2 * (operand_bytes(chunks, max_rank) + exponent_bytes(chunks)) + grad_part_bytes(T, out, in, max_rank);
 }
 
 // (what the standard library throws here is a lack of host memory)

@@ -753,138 +753,139 @@ __global__ __launch_bounds__(kPrepThreads) void lora_prep_kernel(const LoraPrepA
 }
 
 constexpr int kGradThreads = kLoraGradWaves * kWave;
+constexpr int kGradPitch = 128 + 16;   // halves: 4 rows apart on banks of their own for the transposing read
 
-// dA or dB of one job: 128 features by 16 RT ranks, summed over one part of the job's tokens.  The tokens are the sum's index, so
-// both operands want 8 tokens of one feature (rank) in a lane: the second comes prepared, of x (dy) a lane loads 16 bytes of 8
-// tokens' rows (256 bytes of a row per instruction) and turns the 8 x 8 block in its registers.  The wavefronts divide the tokens
-// and meet in LDS.  The sums are kept in units of the present 32 tokens' exponent; tokens whose largest value is 2^-64 of the
-// largest so far are below what binary32 would keep of them.
-template <int RT, bool ODD>
-__global__ __launch_bounds__(kGradThreads) void lora_grad_kernel(const LoraGradArgs a) {
-    const int which = (int)blockIdx.z / a.rank_groups, rt0 = (int)blockIdx.z % a.rank_groups * RT;
+// dA or dB of one job: 128 features by 16 RW ranks, summed over one part of the job's tokens.  RW wavefronts with 16 ranks each share a
+// tile of 32 tokens' x (dy); 4 / RW such groups take the tiles in turn and meet in LDS at the end.  The tokens are the sum's index, so
+// both operands want 8 tokens of one feature (rank) in a lane: the second comes prepared, the tile goes through LDS as it is (256 bytes
+// of a row from 16 lanes) and is read transposed.  The sums are kept in units of the present tile's exponent; tiles whose largest value
+// is 2^-64 of the largest so far are below what binary32 would keep of them.
+// Loads are never under a condition (past the end they repeat the last tile's), or the wait for them would be for all.
+template <int RW, bool ODD>
+__global__ __launch_bounds__(kGradThreads, ODD ? 2 : 3) void lora_grad_kernel(const LoraGradArgs a) {
+    constexpr int TW = kLoraGradWaves / RW, N = 8 / RW, kBuffers = RW > 1 ? 2 : 1;   // groups; rows of 4 per wavefront and tile
+    typedef _Float16 Tile[32][kGradPitch];
+    constexpr size_t kTiles = sizeof(Tile) * TW * kBuffers, kSums = sizeof(float) * kLoraGradWaves * 8 * 4 * kWave;
+    __shared__ __align__(16) char lds[kTiles > kSums ? kTiles : kSums];
+    __shared__ uint16_t ids[kLoraPartTokens];
+    const int which = (int)blockIdx.z / a.rank_groups, rt0 = (int)blockIdx.z % a.rank_groups * RW;
     const LoraGradSide& side = a.side[which];
     int which_job = 0;
 #pragma unroll
     for (int k = 1; k < kLoraGradJobs; ++k) which_job += (int)blockIdx.y >= a.part_begin[k] ? 1 : 0;
     const LoraGradJob& job = a.job[which_job];
-    const int token_parts = job.parts, split = blockIdx.y - a.part_begin[which_job], rank_all = job.rank, count = job.count, first = job.first;
+    const int split = blockIdx.y - a.part_begin[which_job], rank_all = job.rank;
     float* const result = job.out[which];
     const int64_t F = side.F, f0 = (int64_t)blockIdx.x * kLoraFeatures;
     if (!result || 16 * rt0 >= rank_all || f0 >= F) return;
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
-    const int64_t base = min(f0, max(F - kLoraFeatures, (int64_t)0)), fl = base + 8 * m;   // the last 128 features end with the row
-    const int steps = (count + 31) / 32, parts = token_parts * kLoraGradWaves, part = split * kLoraGradWaves + wave;
-    const int s0 = (int)((int64_t)steps * part / parts), s1 = (int)((int64_t)steps * (part + 1) / parts);
-    const bool vectors = !ODD || F >= kLoraFeatures;
-    const int64_t back = fl < F ? 0 : fl - (F - 1);
-    // Of steps s, s + 1: rows are asked for two steps ahead, the prepared operand one.  Loads are never under a condition (past the end
-    // they repeat the last step's), or the wait for them would be for all.
-    half8 rows[2][8], op[2][2 * RT];
-    int exponent[2] = {};
-    typedef const __attribute__((address_space(4))) int32_t* scalar_ints;   // read by scalar loads, which vector loads need not wait for
-    auto load_rows = [&](int buffer, int step) {   // tokens beyond the last repeat the step's first
-        const int s = min(step, s1 - 1);
-        int p[8];
-        if (a.order) {
-            const scalar_ints ids = (scalar_ints)(a.order + first + 32 * s);
-            int id[32];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, group = wave / RW, rank_wave = wave % RW;
+    const int n = lane & 15, q = lane >> 4;
+    // the part's tokens, t0 .. t0 + count - 1 of the job; whole tiles of 32 but for the job's last
+    const int chunks_all = (job.count + 31) / 32, c0 = (int)((int64_t)chunks_all * split / job.parts), c1 = (int)((int64_t)chunks_all * (split + 1) / job.parts);
+    const int t0 = 32 * c0, count = min(32 * c1, job.count) - t0, chunks = c1 - c0;
+    for (int i = threadIdx.x; i < 32 * chunks; i += kGradThreads) {   // (behind the last token: the first once more)
+        const int p = job.first + t0 + (i < count ? i : 0);
+        ids[i] = (uint16_t)(a.order ? a.order[p] : p);
+    }
+    __syncthreads();
+
+    const int64_t base = min(f0, max(F - kLoraFeatures, (int64_t)0)), fl = base + 8 * n;   // the last 128 features end with the row
+    const uint16_t* const d = side.d + (ODD && fl >= F ? F - 1 : fl);
+    const int64_t last = ODD ? max(F - 1 - fl, (int64_t)0) : 7;
+    half8 rows[2][N], op[2][2];
+    int exponent[2];
+    const int mine = rank_wave * 4 * N + q;   // the lane's rows of a tile: mine, mine + 4, ...
+    auto chunk_at = [&](int k) { return min(TW * k + group, chunks - 1); };
+    auto load_rows = [&](int buffer, int k) {
+        const uint16_t* const id = ids + 32 * chunk_at(k) + mine;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) id[i] = 32 * s + i < count ? ids[i] : ids[0];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = g == 0 ? id[i] : g == 1 ? id[8 + i] : g == 2 ? id[16 + i] : id[24 + i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = first + (32 * s + 8 * g + i < count ? 32 * s + 8 * g + i : 32 * s);
-        }
-        if (vectors) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rows[buffer][i] = load8(side.d + p[i] * F + fl);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rows[buffer][i] = load8_each(side.d + p[i] * F + fl - back, F - 1 - fl + back);
+        for (int i = 0; i < N; ++i) {
+            const uint16_t* const p = d + (int64_t)id[4 * i] * F;
+            rows[buffer][i] = !ODD || F >= kLoraFeatures ? load8(p) : load8_each(p, last);
         }
     };
-    auto load_operand = [&](int buffer, int step) {
-        const int chunk = job.chunk_begin + min(step, s1 - 1);
-        exponent[buffer] = ((scalar_ints)side.exponent)[chunk];
-        const half8* const p = side.operand + ((int64_t)chunk * (a.ld / 16) + rt0) * 2 * kWave + lane;
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {   // (rank tiles beyond the job's repeat its last)
-            const int t = min(r, (rank_all - 1) / 16 - rt0);
-            op[buffer][2 * r] = p[2 * t * kWave];
-            op[buffer][2 * r + 1] = p[(2 * t + 1) * kWave];
-        }
+    typedef const __attribute__((address_space(4))) int32_t* scalar_ints;
+    auto load_operand = [&](int buffer, int k) {   // (a wavefront without ranks takes the last's)
+        const int chunk = job.chunk_begin + c0 + chunk_at(k), rt = min(rt0 + rank_wave, (rank_all - 1) / 16);
+        exponent[buffer] = ((scalar_ints)side.exponent)[__builtin_amdgcn_readfirstlane(chunk)];
+        const half8* const p = side.operand + ((int64_t)chunk * (a.ld / 16) + rt) * 2 * kWave + lane;
+        op[buffer][0] = p[0];
+        op[buffer][1] = p[kWave];
     };
-    float4v acc[8][RT] = {};
+    float4v acc[8] = {};
     int e = -200, largest = -200;   // none yet
-    auto product = [&](auto which_buffer, int s) {
+    auto step = [&](auto which_buffer, int k) {
         constexpr int b = decltype(which_buffer)::value;
-        load_operand(1 - b, s + 1);
-        const int now = exponent[b];
-        if (32 * s + 32 > count) {
+        Tile& tile = ((Tile*)lds)[(RW > 1 ? b : 0) * TW + group];
+        const int chunk = TW * k + group;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) rows[b][i] = 32 * s + 8 * g + i < count ? rows[b][i] : half8{};
+        for (int i = 0; i < N; ++i) {
+            const int row = mine + 4 * i;
+            *(half8*)&tile[row][8 * n] = 32 * chunk + row < count ? rows[b][i] : half8{};   // (beyond the part's last tile: all zeros)
         }
-        half8 dv[8];
-        transpose8(rows[b], dv);
-        load_rows(b, s + 2);
-        if (now < largest - 64) {   // too small to count
-#pragma unroll
-            for (int j = 0; j < 8; ++j) dv[j] = half8{};
-        } else {
+        load_rows(b, k + 2);
+        load_operand(1 - b, k + 1);
+        if constexpr (RW > 1)
+            __syncthreads();
+        else
+            __builtin_amdgcn_wave_barrier();
+        const int now = exponent[b];
+        if (now >= largest - 64) {
             largest = max(largest, now);
             if (now != e && e > -200) {
                 const float f = e - now < -126 ? 0.0f : power_of_two(e - now);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) acc[j][r] *= f;
+                for (int j = 0; j < 8; ++j) acc[j] *= f;
             }
             e = now;
+        } else {   // too small to count
+            op[b][0] = half8{};
+            op[b][1] = half8{};
         }
 #pragma unroll
-        for (int r = 0; r < 2 * RT; ++r)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j][r / 2] = mfma(dv[j], op[b][r], acc[j][r / 2]);
+        for (int j = 0; j < 8; ++j) {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s4 lds4;
+            const _Float16* const p = &tile[8 * q + (n >> 2)][16 * j + 4 * (n & 3)];
+            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 4 * kGradPitch));
+            half8 v;
+            __builtin_memcpy(&v, &lo, 8);
+            __builtin_memcpy((char*)&v + 8, &hi, 8);
+            acc[j] = mfma(v, op[b][0], acc[j]);
+            acc[j] = mfma(v, op[b][1], acc[j]);
+        }
     };
-    if (s0 < s1) {
-        load_operand(0, s0);
-        load_rows(0, s0);
-        load_rows(1, s0 + 1);
-        int s = s0;
-        for (; s + 2 <= s1; s += 2) {
-            product(std::integral_constant<int, 0>{}, s);
-            product(std::integral_constant<int, 1>{}, s + 1);
-        }
-        if (s < s1) product(std::integral_constant<int, 0>{}, s);
+    load_operand(0, 0);
+    load_rows(0, 0);
+    load_rows(1, 1);
+    for (int k = 0; TW * k < chunks; k += 2) {   // (of the whole workgroup; steps beyond the last bring zeros)
+        step(std::integral_constant<int, 0>{}, k);
+        step(std::integral_constant<int, 1>{}, k + 1);
     }
     const float up = e > -200 ? power_of_two(e) : 0.0f;
-    __shared__ float sum[kLoraGradWaves][8][4][kWave];   // [wave][j][i][lane (n, q)] = feature 8 (4 q + i) + j, rank n
+    __syncthreads();
+    auto* const sum = (float(*)[8][4][kWave])lds;   // [wave][j][i][lane (n, q)] = feature 16 j + 4 q + i, rank n
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[wave][j][i][lane] = acc[j][i] * up;
+    __syncthreads();
     const float scale = side.scale ? side.scale[job.tenant] : 1.0f;
-    float* const out = token_parts > 1 ? side.partial + (job.partial + (int64_t)split * rank_all) * F : result;
-    const bool add = a.accumulate && token_parts == 1;
+    float* const out = job.parts > 1 ? side.partial + (job.partial + (int64_t)split * rank_all) * F : result;
+    const bool add = a.accumulate && job.parts == 1;
+    constexpr int kRanks = 16 * RW;
+#pragma unroll 4
+    for (int k = 0; k < kRanks * kLoraFeatures / kGradThreads; ++k) {
+        const int at = threadIdx.x + k * kGradThreads;
+        const int r = which == 0 ? at / kLoraFeatures : at % kRanks, f = which == 0 ? at % kLoraFeatures : at / kRanks;
+        const int rank = 16 * rt0 + r;
+        if (rank >= rank_all || base + f < f0 || base + f >= F) continue;
+        float v = 0.0f;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        if (16 * (rt0 + r) >= rank_all) continue;   // (of the whole workgroup)
-        if (r > 0) __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[wave][j][i][lane] = acc[j][r][i] * up;
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 16 * kLoraFeatures / kGradThreads; ++k) {
-            const int at = threadIdx.x + k * kGradThreads;   // of 16 x 128
-            const int n = which == 0 ? at / kLoraFeatures : at & 15, f = which == 0 ? at % kLoraFeatures : at >> 4;
-            const int row = f >> 3, j = f & 7, rank = 16 * (rt0 + r) + n;
-            if (rank >= rank_all || base + f < f0 || base + f >= F) continue;
-            float v = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kLoraGradWaves; ++w) v += sum[w][j][row & 3][16 * (row >> 2) + n];
-            v *= scale;
-            float* const p = out + (which == 0 ? (int64_t)rank * F + base + f : (base + f) * rank_all + rank);
-            *p = add ? *p + v : v;
-        }
+        for (int w = 0; w < TW; ++w) v += sum[w * RW + (r >> 4)][f >> 4][f & 3][16 * ((f >> 2) & 3) + (r & 15)];
+        v *= scale;
+        float* const p = out + (which == 0 ? (int64_t)rank * F + base + f : (base + f) * rank_all + rank);
+        *p = add ? *p + v : v;
     }
 }
 
@@ -952,19 +953,19 @@ hipError_t launch_lora_prep(const LoraPrepArgs& a, int chunks, int sides, hipStr
 }
 
 hipError_t launch_lora_grad(const LoraGradArgs& a, int max_rank, hipStream_t st) {
-    const int rank_tiles = (max_rank + 15) / 16, RT = rank_tiles >= 3 ? 4 : rank_tiles;
+    const int rank_tiles = (max_rank + 15) / 16, RW = lora_grad_rank_waves(max_rank);
     const int64_t F = std::max(a.side[0].F, a.side[1].F), groups = (F + kLoraFeatures - 1) / kLoraFeatures;
     if (a.n_jobs < 1 || rank_tiles < 1 || groups < 1 || a.n_parts < 1) return hipErrorInvalidValue;
     LoraGradArgs b = a;
-    b.rank_groups = (rank_tiles + RT - 1) / RT;
+    b.rank_groups = (rank_tiles + RW - 1) / RW;
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)b.n_parts, (unsigned)(2 * b.rank_groups)), dim3(kGradThreads), 0, st, b);
         return hipGetLastError();
     };
     // rows below 128 elements (a side that is not wanted has none)
     const bool odd = (a.side[0].F > 0 && a.side[0].F < kLoraFeatures) || (a.side[1].F > 0 && a.side[1].F < kLoraFeatures);
-    if (odd) return RT == 1 ? go(lora_grad_kernel<1, true>) : RT == 2 ? go(lora_grad_kernel<2, true>) : go(lora_grad_kernel<4, true>);
-    return RT == 1 ? go(lora_grad_kernel<1, false>) : RT == 2 ? go(lora_grad_kernel<2, false>) : go(lora_grad_kernel<4, false>);
+    if (odd) return RW == 1 ? go(lora_grad_kernel<1, true>) : RW == 2 ? go(lora_grad_kernel<2, true>) : go(lora_grad_kernel<4, true>);
+    return RW == 1 ? go(lora_grad_kernel<1, false>) : RW == 2 ? go(lora_grad_kernel<2, false>) : go(lora_grad_kernel<4, false>);
 }
 
 hipError_t launch_lora_reduce(const LoraReduceArgs& a, int64_t max_n, hipStream_t st) {

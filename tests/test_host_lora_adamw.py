@@ -33,9 +33,9 @@ def test_workspace_sizes(bd):
     assert f(100, 3, 17) == 512 + 8 * 3 * 100 * 32 * 4
     assert f(65535, 1, 256) == 262144 + 65535 * 256 * 4
     assert f(0, 1, 8) == 0 and f(1, 4, 8) == 0 and f(1, 0, 8) == 0 and f(1, 1, 0) == 0 and f(1, 1, 257) == 0 and f(65536, 1, 1) == 0
-    # g and h as operands (2 KB per 16 ranks and chunk of 32 tokens; 3 chunks and one more per tenant), a number per chunk, and 16 parts
-    # of the gradients of one adapter
-    assert b(100, 40, 64, 5, 17) == 512 + 8 * 100 * 32 * 4 + 2 * (8 * 2 * 2048 + 256) + 16 * 32 * (40 + 64) * 4
+    # g and h as operands (2 KB per 16 ranks and chunk of 32 tokens; 3 chunks and one more per tenant), a number per chunk, and 3 parts
+    # of the gradients of one adapter (one for 32 tokens, 32 at most)
+    assert b(100, 40, 64, 5, 17) == 512 + 8 * 100 * 32 * 4 + 2 * (8 * 2 * 2048 + 256) + 3 * 32 * (40 + 64) * 4
     assert b(0, 40, 64, 1, 17) == 0 and b(1, 40, 65, 1, 17) == 0 and b(1, -1, 64, 1, 1) == 0 and b(1, 40, 64, 1, 0) == 0 and b(1, 40, 64, 0, 1) == 0
 
 
