@@ -29,6 +29,15 @@ struct LoraTile {                       // few tokens
     uint16_t rank, count, mat, unused;
     uint32_t col[8];                    // the tokens, two per word
 };
+struct LoraDecodeTile {                 // a few tokens of a tenant, low ranks: both products in one launch
+    const uint16_t *wa, *wb;
+    int32_t tenant;
+    uint16_t rank, count, mat, unused;
+    uint16_t col[4];
+};
+constexpr int kLoraDecodeTokens = 4, kLoraDecodeRank = 32;   // at most, of such a tile
+constexpr int kLoraDecodeFeatures = 1024;                    // of a workgroup
+
 struct LoraJob {                        // many tokens
     const uint16_t* w;
     int32_t hrow, tenant, count;
@@ -71,6 +80,18 @@ struct LoraExpandArgs {
         LoraTile tile[kLoraRecords];
         LoraJobs jobs;
     };
+};
+
+struct LoraDecodeArgs {
+    const uint16_t* x;                  // [T, in]
+    const uint16_t* y0[kLoraMaxMats];   // may be nullptr
+    uint16_t* y[kLoraMaxMats];
+    const float* scale[kLoraMaxMats];
+    float* h_out[kLoraMaxMats];         // may be nullptr
+    int64_t F[kLoraMaxMats];
+    int64_t in;
+    int32_t n_tiles, h_ld;
+    LoraDecodeTile tile[kLoraRecords];
 };
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -126,6 +147,7 @@ constexpr int lora_shrink_groups(int rank, int columns) { return (rank + 15) / 1
 
 // `columns`: tokens of a tile (16: records are tiles; else records are jobs, 64).  max_rank: the largest rank of the records;
 // odd: some rank is not a multiple of 8 (B's rows are then no whole 16-byte pieces).
+hipError_t launch_lora_decode(const LoraDecodeArgs& a, int max_tokens, int64_t max_F, bool odd, hipStream_t st);
 hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transposed, int max_rank, bool odd, hipStream_t st);
 hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int max_rank, int64_t min_F, int64_t max_F, bool odd, hipStream_t st);
 // prepares `chunks` chunks from a.chunk_first on, of `sides` sides from a.side_first on

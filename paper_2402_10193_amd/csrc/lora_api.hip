@@ -16,6 +16,7 @@ using bd::overlaps;
 
 constexpr int kFewColumns = 16, kManyColumns = bd::kLoraExpandTokens;   // tokens of a tile: records are tiles, or jobs
 constexpr int64_t kFewTokens = 512;                  // largest batch whose records are tiles
+constexpr int64_t kDecodeBytes = 256 << 10;          // of A, that every workgroup of a decode launch reads
 constexpr int kGradParts = 32;                       // parts of jobs whose tokens are in more than one, of all jobs together
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
@@ -140,6 +141,15 @@ bool sizes_ok(int64_t T, int64_t out, int64_t in, int32_t n_tenants) {
     return T >= 0 && T <= 65535 && out >= 0 && in >= 0 && n_tenants >= 0 && in % 32 == 0 && out <= (int64_t)1 << 24 && in <= (int64_t)1 << 24;
 }
 
+// Both products in one launch (lora_decode_kernel), where it is quicker: a few tokens of every tenant, low ranks, and an A that every workgroup
+// can read again: TODO measured.
+bool decode_fits(const Batch& b, int max_rank, int64_t in) {
+    if (max_rank > bd::kLoraDecodeRank || in < 8 || (int64_t)max_rank * in * 2 > kDecodeBytes) return false;
+    for (const Job& j : b.jobs)
+        if (j.count > bd::kLoraDecodeTokens) return false;
+    return true;
+}
+
 bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by, const uint16_t* const* b_by, const int32_t* rank_by,
                   const float* const* scale, const int32_t* tenant_of_token, const uint16_t* const* y0, uint16_t* const* y,
                   float* const* h, int32_t h_ld, int64_t T, const int64_t* out, int64_t in, int32_t n_tenants, void* workspace,
@@ -196,7 +206,43 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
         }
     if (max_rank > 0 && (!workspace || workspace_bytes < order_bytes(T) + h_bytes(T, n_mats, max_rank) || misaligned(workspace, 256)))
         return BD_ERR_WORKSPACE;
+    // without an adapter there is nothing to do where y is y0
+    auto takes_part = [&](int m, int32_t rank) { return (out[m] > 0 || (h && h[m])) && (rank > 0 || !(y0 && y0[m] == y[m])); };
     // ---- checked: launches from here on ----
+    if (decode_fits(batch, max_rank, in)) {
+        auto d = std::make_unique<bd::LoraDecodeArgs>();
+        for (int m = 0; m < n_mats; ++m) {
+            d->y0[m] = y0 ? y0[m] : nullptr;
+            d->y[m] = y[m];
+            d->scale[m] = scale[m];
+            d->F[m] = out[m];
+            d->h_out[m] = h ? h[m] : nullptr;
+        }
+        d->x = x;
+        d->in = in;
+        d->h_ld = h_ld;
+        int tokens = 1;
+        bool odd = false;
+        auto flush = [&]() {
+            const bool ok = d->n_tiles == 0 || bd::launch_lora_decode(*d, tokens, max_out, odd, st) == hipSuccess;
+            d->n_tiles = 0;
+            tokens = 1;
+            odd = false;
+            return ok;
+        };
+        for (const Job& j : batch.jobs)
+            for (int m = 0; m < n_mats; ++m) {
+                const size_t at = (size_t)m * n_tenants + j.tenant;
+                if (!takes_part(m, rank_by[at])) continue;
+                bd::LoraDecodeTile& t = d->tile[d->n_tiles++];
+                t = bd::LoraDecodeTile{a_by[at], b_by[at], j.tenant, (uint16_t)rank_by[at], (uint16_t)j.count, (uint16_t)m, 0, {0, 0, 0, 0}};
+                for (int c = 0; c < j.count; ++c) t.col[c] = (uint16_t)batch.token(j.first + c);
+                tokens = std::max(tokens, (int)j.count);
+                odd |= rank_by[at] % 8 != 0;
+                if (d->n_tiles == bd::kLoraRecords && !flush()) return BD_ERR_DEVICE;
+            }
+        return flush() ? BD_OK : BD_ERR_DEVICE;
+    }
     const bool few = T <= kFewTokens;
     const int columns = few ? kFewColumns : kManyColumns;
     const int32_t* order = nullptr;
@@ -251,8 +297,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
             const size_t at = (size_t)m * n_tenants + tenant;
             *w = b_by[at];
             *rank = rank_by[at];
-            // without an adapter there is nothing to do where y is y0
-            return (out[m] > 0 || (h && h[m])) && (rank_by[at] > 0 || !(y0 && y0[m] == y[m]));
+            return takes_part(m, rank_by[at]);
         },
         [&](int rank, bool odd) { return bd::launch_lora_expand(*x2, columns, false, rank, min_out, max_out, odd, st); });
     return e == hipSuccess ? BD_OK : BD_ERR_DEVICE;

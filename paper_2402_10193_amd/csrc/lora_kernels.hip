@@ -131,6 +131,118 @@ __device__ __forceinline__ void tokens_of(const Args& a, const Where& u, const i
     }
 }
 
+constexpr int kDecodeThreads = 512;
+
+// A decode step: up to 4 tokens of a tenant, up to 32 ranks, both products in one launch, bound by latency.  Every workgroup of 1024
+// features forms all of h (A comes out of the cache again for the next one): a launch and the way of h through memory would take longer.
+// Vector arithmetic: a wavefront reads rows of A as they are, 1 KB of a row per instruction, and a lane the rows of B of its two features;
+// the matrix cores' order would take the address unit four times as long.  y0 and B are asked for before h is formed.
+template <int TOK, bool ODD>
+__global__ __launch_bounds__(kDecodeThreads) void lora_decode_kernel(const LoraDecodeArgs a) {
+    constexpr int kWaves = kDecodeThreads / kWave, kOctets = kLoraDecodeRank / 8, kRows = kLoraDecodeRank / kWaves, kSegments = 8, kFeatures = kLoraDecodeFeatures / kDecodeThreads;
+    __shared__ __align__(16) float h[TOK][kLoraDecodeRank];
+    const LoraDecodeTile& k = a.tile[blockIdx.x];
+    const int rank = k.rank, count = k.count, mat = k.mat;
+    const int64_t F = a.F[mat], base = (int64_t)blockIdx.y * kLoraDecodeFeatures;
+    if (blockIdx.y > 0 && base >= F) return;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    int64_t token[TOK];
+#pragma unroll
+    for (int t = 0; t < TOK; ++t) token[t] = k.col[t < count ? t : 0];
+    const uint16_t* const y0 = a.y0[mat];
+    const bool work = base < F;   // (not for a matrix without outputs, whose h alone is asked for)
+
+    _Float16 before[kFeatures][TOK];
+    half8 b[kFeatures][kOctets];
+    if (work) {
+#pragma unroll
+        for (int i = 0; i < kFeatures; ++i) {
+            const int64_t f = min(base + i * kDecodeThreads + (int)threadIdx.x, F - 1);
+#pragma unroll
+            for (int t = 0; t < TOK; ++t) before[i][t] = y0 ? *(const _Float16*)(y0 + token[t] * F + f) : (_Float16)0.0f;
+            const uint16_t* const row = k.wb + f * rank;
+#pragma unroll
+            for (int o = 0; o < kOctets; ++o)
+                if (8 * o < rank) {
+                    if (!ODD || 8 * o + 8 <= rank)
+                        b[i][o] = load8(row + 8 * o);
+                    else
+                        b[i][o] = load8_each(row + 8 * o, rank - 1 - 8 * o);
+                }
+        }
+    }
+
+    // h: row by row of A, rows wave, wave + 8, ...; two rows at a time
+#pragma unroll
+    for (int i0 = 0; i0 < kRows; i0 += 2) {
+        if (wave + kWaves * i0 >= rank) continue;   // (of the whole wavefront)
+        float sum[2][TOK] = {};
+        const uint16_t* row[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) row[i] = k.wa + (int64_t)min(wave + kWaves * (i0 + i), rank - 1) * a.in;
+        for (int64_t k0 = 8 * lane; k0 < a.in + 8 * lane; k0 += 512 * kSegments) {
+            half8 av[2][kSegments], xv[TOK][kSegments];
+#pragma unroll
+            for (int g = 0; g < kSegments; ++g) {   // (behind the row: its last elements, which count as zeros)
+                const int64_t at = min(k0 + 512 * g, a.in - 8);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) av[i][g] = load8(row[i] + at);
+#pragma unroll
+                for (int t = 0; t < TOK; ++t) xv[t][g] = load8(a.x + token[t] * a.in + at);
+            }
+#pragma unroll
+            for (int g = 0; g < kSegments; ++g) {
+                const bool real = k0 + 512 * g < a.in;
+#pragma unroll
+                for (int t = 0; t < TOK; ++t)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float s = 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) s = __builtin_fmaf((float)av[i][g][e], (float)xv[t][g][e], s);
+                        sum[i][t] += real ? s : 0.0f;
+                    }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int t = 0; t < TOK; ++t) {
+                const float v = wave_sum(sum[i][t]);
+                const int r = wave + kWaves * (i0 + i);
+                if (lane == 0 && r < rank) h[t][r] = v;
+            }
+    }
+    __syncthreads();
+    if (a.h_out[mat] && blockIdx.y == 0) {
+        const int t = threadIdx.x / kLoraDecodeRank, r = threadIdx.x % kLoraDecodeRank;
+        if (t < count && r < rank) a.h_out[mat][(int64_t)k.col[t] * a.h_ld + r] = h[t][r];
+    }
+    if (!work) return;
+    const float scale = rank > 0 ? a.scale[mat][k.tenant] : 0.0f;
+    float sum[kFeatures][TOK] = {};
+#pragma unroll
+    for (int o = 0; o < kOctets; ++o)
+        if (8 * o < rank) {
+#pragma unroll
+            for (int t = 0; t < TOK; ++t)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!ODD || 8 * o + e < rank) {
+                        const float v = h[t][8 * o + e];
+#pragma unroll
+                        for (int i = 0; i < kFeatures; ++i) sum[i][t] = __builtin_fmaf((float)b[i][o][e], v, sum[i][t]);
+                    }
+        }
+#pragma unroll
+    for (int i = 0; i < kFeatures; ++i) {
+        const int64_t f = base + i * kDecodeThreads + threadIdx.x;
+#pragma unroll
+        for (int t = 0; t < TOK; ++t)
+            if (f < F && t < count) *(_Float16*)(a.y[mat] + token[t] * F + f) = (_Float16)__builtin_fmaf(sum[i][t], scale, (float)before[i][t]);
+    }
+}
+
 constexpr int kShrinkThreads = kLoraShrinkWaves * kWave;
 
 // A wavefront's own piece of LDS, 32 rows of 16 RT ranks of B (B [K, rank] has the sum's index outside): stored as rows, read back
@@ -172,7 +284,7 @@ struct Turn {
 };
 
 // h = A x or g = s B^T dy of one tile, 16 RT ranks and one part of the sum.  The wavefronts divide the part among them, their
-// sums meet in LDS.  Of one tile of 16 tokens x (and A) is read straight into matrix-core order, which is less to wait for.
+// sums meet in LDS. 
 // Ranks and columns beyond the last repeat others or hold anything: rows and columns do not mix, and what they give is not kept.
 template <bool TR, int NT, int RT, bool ODD>
 __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraShrinkArgs a) {
@@ -180,8 +292,7 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
     const int rt0 = blockIdx.z * RT;
     if (16 * rt0 >= u.rank) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
-    constexpr bool kMoved = NT > 1;
-    const int mr = kMoved ? lane >> 2 : m, mp = kMoved ? lane & 3 : g;   // the row and the 16 bytes of 64 that the lane loads
+    const int mr = lane >> 2, mp = lane & 3;   // the row and the 16 bytes of 64 that the lane loads
     const uint16_t* row[NT];
     int column[NT], token[NT];
 #pragma unroll
@@ -190,7 +301,7 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
 #pragma unroll
     for (int n = 0; n < NT; ++n) row[n] = a.src + (int64_t)token[n] * a.K + 8 * mp;
     // a wavefront's piece of LDS takes B, then (A, then) x; at the end all of it takes the sums
-    constexpr size_t kTurn = kMoved ? sizeof(Turn<(NT > RT ? NT : RT)>) : 0, kStage = TR ? sizeof(Stage<RT>) : 0, kMine = kTurn > kStage ? kTurn : kStage;
+    constexpr size_t kTurn = sizeof(Turn<(NT > RT ? NT : RT)>), kStage = TR ? sizeof(Stage<RT>) : 0, kMine = kTurn > kStage ? kTurn : kStage;
     constexpr size_t kSums = sizeof(float4v) * kLoraShrinkWaves * RT * NT * kWave;
     __shared__ __align__(16) char lds[kSums > kLoraShrinkWaves * kMine ? kSums : kLoraShrinkWaves * kMine];
     Stage<RT>& stage = *(Stage<RT>*)(lds + wave * kMine);
@@ -263,14 +374,14 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
 #pragma unroll
             for (int r = 0; r < RT; ++r) wo[r] = stage.operand(r, lane);
             __builtin_amdgcn_wave_barrier();
-        } else if constexpr (kMoved) {
+        } else {
             (*(Turn<RT>*)(lds + wave * kMine))(w, wo, lane);
         }
-        if constexpr (kMoved) (*(Turn<NT>*)(lds + wave * kMine))(x, xo, lane);
+        (*(Turn<NT>*)(lds + wave * kMine))(x, xo, lane);
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) acc[r][n] = mfma(TR || kMoved ? wo[r] : w[r], kMoved ? xo[n] : x[n], acc[r][n]);
+            for (int n = 0; n < NT; ++n) acc[r][n] = mfma(wo[r], xo[n], acc[r][n]);
     };
     // Two buffers; loads are never under a condition (past the end they repeat the last step's), or the wait for them would be for all.
     if (mine > 0) {
@@ -310,7 +421,7 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
     }
     float* const dst = a.h + (int64_t)blockIdx.y * a.split_stride;
     auto* const sum = (float4v(*)[RT * NT][kWave])lds;
-    if constexpr (TR || kMoved) __syncthreads();
+    __syncthreads();
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -330,78 +441,79 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
 }
 
 constexpr int kExpandThreads = kLoraExpandWaves * kWave;
-constexpr int kExpandRanks = 128;   // ranks whose hi and lo are in LDS at a time
 
-// Few tokens: y = y0 + s B h, or dx = dx0 + A^T g, of one tile of 16 tokens by 512 features.  h comes in as `splits` partial sums.  Rows of a result are
-// tokens, columns features: feature 8 n + j of a wavefront's 128 is column n of its MFMA j, so that a lane ends up with 8
-// neighbours of a token's row in its 8 accumulators, and 16 lanes with 256 bytes of the row: one load of y0 and one store for
-// each.  The 32 elements of an MFMA's sum are 16 ranks, hi in lane groups 0 and 1 and lo in 2 and 3, both with the same weights.
+// Few tokens: y = y0 + s B h, or dx = dx0 + A^T g, of one tile of 16 tokens by 512 features, 128 for each wavefront.  h comes in as
+// `splits` partial sums.  Rows of a result are tokens, columns features: feature 8 n + j of a wavefront's 128 is column n of its MFMA
+// j, so that a lane ends up with 8 neighbours of a token's row in its 8 accumulators, and 16 lanes with 256 bytes of the row: one
+// load of y0 and one store for each.  The 32 elements of an MFMA's sum are 16 ranks, hi in lane groups 0 and 1 and lo in 2 and 3, both
+// with the same weights.  Forward a wavefront's weights, 32 ranks of 128 features at a time, are read in runs of neighbouring bytes and
+// come into that order through a piece of LDS of its own (64 bytes a feature, 16 more behind 8 features: no bank conflicts); backward
+// 8 ranks' rows of A are turned in registers.
 // y0 and the first weights are asked for before h is prepared: three waits for memory become one.
+constexpr int kFewStage = 128 * 64 + 16 * 16;   // bytes
 template <bool TR, bool ODD>
 __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const LoraExpandArgs a) {
-    constexpr int NT = 1, kTokens = 16 * NT, kPer = kExpandThreads / kTokens;   // threads per token while h is prepared
-    constexpr int kPitch = kExpandRanks + 8;
-    __shared__ __align__(16) _Float16 hi[kTokens][kPitch], lo[kTokens][kPitch];
+    constexpr int kTokens = 16, kPer = kExpandThreads / kTokens;   // threads per token while h is prepared
+    extern __shared__ __align__(16) char lds[];
     __shared__ float unit[kTokens];
-    const Where u = find_tile<NT>(a, blockIdx.x);
+    const Where u = find_tile<1>(a, blockIdx.x);
     const int64_t F = a.F[u.mat];
     if (blockIdx.y > 0 && (int64_t)blockIdx.y * kLoraExpandWaves * kLoraFeatures >= F) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
-    const int padded = (u.rank + 15) & ~15;
+    const int padded = (u.rank + 15) & ~15, pitch = padded + 8;
+    char* const stage = lds + wave * kFewStage;   // (forward)
+    _Float16* const hi = (_Float16*)(lds + (TR ? 0 : kLoraExpandWaves * kFewStage));
+    _Float16* const lo = hi + kTokens * pitch;
     // the wavefront's features, f0 .. f0 + 127; the last one's 128 end with the row and it keeps what is its own; a row below 128 is
     // read element by element
-    const int64_t f0 = ((int64_t)blockIdx.y * kLoraExpandWaves + wave) * kLoraFeatures, f = min(f0, max(F - kLoraFeatures, (int64_t)0)) + 8 * m;
+    const int64_t f0 = ((int64_t)blockIdx.y * kLoraExpandWaves + wave) * kLoraFeatures, base = min(f0, max(F - kLoraFeatures, (int64_t)0)), f = base + 8 * m;
     const bool active = f0 < F, vectors = !ODD || F >= kLoraFeatures;
 
-    int64_t at[NT][4];   // the rows of y that the lane's results belong to: token 16 n + 4 g + i
-    half8 before[NT][4];
-    int column[4 * NT], token[4 * NT];
+    int64_t at[4];   // where the lane's results belong: token 4 g + i
+    half8 before[4];
+    {
+        int column[4], token[4];
 #pragma unroll
-    for (int k = 0; k < 4 * NT; ++k) {
-        const int c = 16 * (k >> 2) + 4 * g + (k & 3);
-        column[k] = c < u.count ? c : 0;
+        for (int i = 0; i < 4; ++i) column[i] = 4 * g + i < u.count ? 4 * g + i : 0;
+        tokens_of<1>(a, u, column, token);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i] = (int64_t)token[i] * F + f;
     }
-    tokens_of<NT>(a, u, column, token);
-#pragma unroll
-    for (int k = 0; k < 4 * NT; ++k) at[k >> 2][k & 3] = (int64_t)token[k] * F + f;
     const uint16_t* const y0 = active ? a.y0[u.mat] : nullptr;
     if (y0 && vectors) {
 #pragma unroll
-        for (int k = 0; k < 4 * NT; ++k) before[k >> 2][k & 3] = load8(y0 + at[k >> 2][k & 3]);
+        for (int i = 0; i < 4; ++i) before[i] = load8(y0 + at[i]);
     } else if (ODD && y0) {
         const int64_t back = f < F ? 0 : f - (F - 1);   // a lane behind the row reads its last element
 #pragma unroll
-        for (int k = 0; k < 4 * NT; ++k) before[k >> 2][k & 3] = load8_each(y0 + at[k >> 2][k & 3] - back, F - 1 - f + back);
+        for (int i = 0; i < 4; ++i) before[i] = load8_each(y0 + at[i] - back, F - 1 - f + back);
     } else {
 #pragma unroll
-        for (int k = 0; k < 4 * NT; ++k) before[k >> 2][k & 3] = half8{};
+        for (int i = 0; i < 4; ++i) before[i] = half8{};
     }
-    half8 wv[8];   // forward: the weights of 16 ranks; backward: 8 ranks' rows of A, still to be turned
+    // Forward: lane and instruction i have piece q = 64 i + lane, 8 ranks of feature q / per_row; the last 8 of a rank that is no multiple of
+    // 8 end with it.  Backward: 8 ranks' rows of A.
+    half8 wv[8];
+    auto per_row = [&](int r) { return (min(32, u.rank - r) + 7) / 8; };
+    auto piece_row = [&](int i, int n) { return (int)(((unsigned)(kWave * i + lane) * (65536u / (unsigned)n + 1)) >> 16); };
+    auto piece_rank = [&](int i, int n, int r) {
+        const int rank = r + 8 * (kWave * i + lane - piece_row(i, n) * n);
+        return ODD ? min(rank, max(u.rank - 8, 0)) : rank;
+    };
     auto load_weights = [&](int r) {
-        const int rank = r + 8 * (g & 1), left = u.rank - rank;
         if constexpr (TR) {
+            const int rank = r + 8 * (g & 1), left = u.rank - rank;
             const uint16_t* const w = u.w + (f <= F - 8 ? f : F - 8);   // (F = in, a multiple of 32)
 #pragma unroll
             for (int i = 0; i < 8; ++i) wv[i] = load8(w + (int64_t)(i < left ? rank + i : u.rank - 1) * F);
-            if (u.rank - r < 16) {   // rows beyond the rank repeat the last one: they do not count
-#pragma unroll
-                for (int i = 0; i < 8; ++i) wv[i] = i < left ? wv[i] : half8{};
-            }
         } else {
-            const uint16_t* w[8];
+            const int n = per_row(r);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = u.w + (f + j < F ? f + j : F - 1) * u.rank;
-            if (!ODD || u.rank % 8 == 0) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) wv[j] = load8(w[j] + (left > 0 ? rank : r));
-                if (u.rank - r < 16) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) wv[j] = left > 0 ? wv[j] : half8{};
+            for (int i = 0; i < 8; ++i)
+                if (i < 2 * n) {
+                    const uint16_t* const w = u.w + min(base + piece_row(i, n), F - 1) * u.rank;
+                    wv[i] = !ODD || u.rank >= 8 ? load8(w + piece_rank(i, n, r)) : load8_each(w, u.rank - 1);
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) wv[j] = only(load8_each(w[j] + (left > 0 ? rank : r), left > 0 ? left - 1 : 0), 0, left);
-            }
         }
     };
     if (active && padded > 0) load_weights(0);
@@ -418,10 +530,12 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
         for (int s = 1; s < kLoraMaxSplits; ++s) v += part[s];
         return v;
     };
+    float* const kept = !TR && a.h_out[u.mat] && blockIdx.y == 0 && real ? a.h_out[u.mat] + (int64_t)token_of<1>(a, u, c) * a.h_ld : nullptr;
     float top = 0.0f;
-    float* const kept = !TR && a.h_out[u.mat] && blockIdx.y == 0 && real ? a.h_out[u.mat] + (int64_t)token_of<NT>(a, u, c) * a.h_ld : nullptr;
+    float4v first = {};   // of the thread's first four ranks: all there are up to 64
     for (int r = 4 * sub; r < padded; r += 4 * kPer) {
         const float4v v = sum4(r);
+        if (r == 4 * sub) first = v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             top = fmaxf(top, finite_abs(v[i]));
@@ -431,64 +545,91 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
 #pragma unroll
     for (int d = kPer / 2; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
     const int e = group_exponent(top);
-    if (sub == 0) unit[c] = power_of_two(e);
+    if (sub == 0) unit[c] = power_of_two(e) * (TR || u.rank == 0 ? 1.0f : a.scale[u.mat][u.tenant]);
     const float down = power_of_two(-e);
-
-    float4v acc[8][NT] = {};
-    for (int r0 = 0; r0 < padded; r0 += kExpandRanks) {
-        const int ranks = min(kExpandRanks, padded - r0);
-        if (r0 > 0) __syncthreads();
-        for (int r = 4 * sub; r < ranks; r += 4 * kPer) {
-            const float4v v = sum4(r0 + r);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                _Float16 h = (_Float16)0.0f, l = (_Float16)0.0f;
-                if (real) split_half(v[i], down, &h, &l);
-                hi[c][r + i] = h;
-                lo[c][r + i] = l;
-            }
-        }
-        __syncthreads();
-        if (!active) continue;
-        for (int rc = 0; rc < ranks; rc += 16) {
-            half8 cols[8];
-            if constexpr (TR) {
-                transpose8(wv, cols);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) cols[j] = wv[j];
-            }
-            if (r0 + rc + 16 < padded) load_weights(r0 + rc + 16);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const half8 hv = *(const half8*)(g < 2 ? &hi[16 * n + m][rc + 8 * g] : &lo[16 * n + m][rc + 8 * (g - 2)]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j][n] = mfma(hv, cols[j], acc[j][n]);
-            }
-        }
-    }
-    if (padded == 0) __syncthreads();   // `unit`
-    if (!active) return;
-    const float scale = TR || u.rank == 0 ? 1.0f : a.scale[u.mat][u.tenant];
-    uint16_t* const y = a.y[u.mat];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int r = 4 * sub; r < padded; r += 4 * kPer) {
+        const float4v v = r == 4 * sub ? first : sum4(r);
+        half4 h, l;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int col = 16 * n + 4 * g + i;
-            if (col >= u.count || f >= F) continue;
-            const float up = unit[col] * scale;
-            half8 v;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (_Float16)__builtin_fmaf(acc[j][n][i], up, (float)before[n][i][j]);
-            if (f >= f0 && F - f >= 8) {
-                __builtin_memcpy(y + at[n][i], &v, 16);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (f + j >= f0 && f + j < F) *(_Float16*)(y + at[n][i] + j) = v[j];
-            }
+            _Float16 p, q;
+            split_half(v[i], down, &p, &q);
+            h[i] = real ? p : (_Float16)0.0f;
+            l[i] = real ? q : (_Float16)0.0f;
         }
+        *(half4*)(hi + c * pitch + r) = h;
+        *(half4*)(lo + c * pitch + r) = l;
+    }
+    __syncthreads();
+    if (!active) return;
+
+    const _Float16* const mine = (g < 2 ? hi : lo) + m * pitch + 8 * (g & 1);
+    float4v acc[8] = {};
+    auto product = [&](const half8 (&cols)[8], int r) {
+        const half8 hv = *(const half8*)(mine + r);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = mfma(hv, cols[j], acc[j]);
+    };
+    for (int r0 = 0; r0 < padded; r0 += TR ? 16 : 32) {
+        if constexpr (TR) {
+            half8 cols[8];
+            if (u.rank - r0 < 16) {   // rows beyond the rank repeat the last one: they do not count
+#pragma unroll
+                for (int i = 0; i < 8; ++i) wv[i] = i < u.rank - r0 - 8 * (g & 1) ? wv[i] : half8{};
+            }
+            transpose8(wv, cols);
+            if (r0 + 16 < padded) load_weights(r0 + 16);
+            product(cols, r0);
+        } else {
+            const int n = per_row(r0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < 2 * n) {
+                    const int row = piece_row(i, n), rank = piece_rank(i, n, r0) - r0;
+                    char* const p = stage + row * 64 + (row >> 3) * 16;
+                    if (!ODD || u.rank % 8 == 0) {
+                        *(half8*)(p + 2 * rank) = wv[i];
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (rank + k >= 0 && rank + k < 32) *(_Float16*)(p + 2 * (rank + k)) = wv[i][k];
+                    }
+                }
+            __builtin_amdgcn_wave_barrier();
+            if (r0 + 32 < padded) load_weights(r0 + 32);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int r = r0 + 16 * half, left = u.rank - r - 8 * (g & 1);
+                if (r >= padded) continue;
+                half8 cols[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) cols[j] = *(const half8*)(stage + m * (8 * 64 + 16) + j * 64 + half * 32 + (g & 1) * 16);
+                if (u.rank - r < 16) {   // what lies beyond the rank does not count
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) cols[j] = ODD ? only(cols[j], 0, left) : left > 0 ? cols[j] : half8{};
+                }
+                product(cols, r);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    uint16_t* const y = a.y[u.mat];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int col = 4 * g + i;
+        if (col >= u.count || f >= F) continue;
+        const float up = unit[col];
+        half8 v;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (_Float16)__builtin_fmaf(acc[j][i], up, (float)before[i][j]);
+        if (f >= f0 && F - f >= 8) {
+            __builtin_memcpy(y + at[i], &v, 16);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (f + j >= f0 && f + j < F) *(_Float16*)(y + at[i] + j) = v[j];
+        }
+    }
 }
 
 // Many tokens: the same of one tile of 64 tokens, 16 for each wavefront, which take 128 features at a time together, gridDim.y of
@@ -901,8 +1042,19 @@ __global__ __launch_bounds__(256) void lora_reduce_kernel(const LoraReduceArgs a
 
 }  // namespace
 
-static_assert(sizeof(LoraShrinkArgs) <= 4096 && sizeof(LoraExpandArgs) <= 4096 && sizeof(LoraGradArgs) <= 4096 && sizeof(LoraReduceArgs) <= 4096 && sizeof(LoraPrepArgs) <= 4096,
+static_assert(sizeof(LoraDecodeArgs) <= 4096 && sizeof(LoraShrinkArgs) <= 4096 && sizeof(LoraExpandArgs) <= 4096 && sizeof(LoraGradArgs) <= 4096 && sizeof(LoraReduceArgs) <= 4096 && sizeof(LoraPrepArgs) <= 4096,
               "kernel arguments");
+
+hipError_t launch_lora_decode(const LoraDecodeArgs& a, int max_tokens, int64_t max_F, bool odd, hipStream_t st) {
+    const int64_t groups = max_F > 0 ? (max_F + kLoraDecodeFeatures - 1) / kLoraDecodeFeatures : 1;   // (F = 0: h alone)
+    if (a.n_tiles < 1 || groups > 65535 || max_tokens > kLoraDecodeTokens || a.in < 8) return hipErrorInvalidValue;
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)groups), dim3(kDecodeThreads), 0, st, a);
+        return hipGetLastError();
+    };
+    if (odd) return max_tokens == 1 ? go(lora_decode_kernel<1, true>) : max_tokens == 2 ? go(lora_decode_kernel<2, true>) : go(lora_decode_kernel<4, true>);
+    return max_tokens == 1 ? go(lora_decode_kernel<1, false>) : max_tokens == 2 ? go(lora_decode_kernel<2, false>) : go(lora_decode_kernel<4, false>);
+}
 
 hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transposed, int max_rank, bool odd, hipStream_t st) {
     const int rank_tiles = (max_rank + 15) / 16;
@@ -925,8 +1077,9 @@ hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transpo
     if (columns == 16) {
         const int64_t groups = (wide + kLoraExpandWaves - 1) / kLoraExpandWaves;
         if (groups > 65535) return hipErrorInvalidValue;
+        const unsigned lds = (unsigned)((transposed ? 0 : kLoraExpandWaves * kFewStage) + 2 * 16 * (((max_rank + 15) & ~15) + 8) * 2);
         auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)groups), dim3(kExpandThreads), 0, st, a);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)groups), dim3(kExpandThreads), lds, st, a);
             return hipGetLastError();
         };
         return transposed ? (odd ? go(lora_expand_few_kernel<true, true>) : go(lora_expand_few_kernel<true, false>)) : odd ? go(lora_expand_few_kernel<false, true>) : go(lora_expand_few_kernel<false, false>);
