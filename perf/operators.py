@@ -369,7 +369,10 @@ def _own_adamw(s):
         more = {} if s["bits"] == 32 else {"exp_avg_scales": scales(s["ms"]), "exp_avg_sq_scales": scales(s["vs"])}
         s["group"] = bd.AdamWGroup(cut(s["p"]), cut(s["g"]), cut(s["m"]), cut(s["v"]), params_f16=cut(s["p16"]), **more)
     bd.adamw(s["group"], s["lr"], s["step"], beta1=BETA1, beta2=BETA2, eps=EPS, weight_decay=DECAY, grad_scale=s["grad_scale"])
-    return {"p": s["p"], "p16": s["p16"], **_states_of(s)}
+    states = {"m": s["m"], "v": s["v"]}
+    if s["bits"] == 8:
+        states = {"m": bd.adamw_values(s["m"], False), "v": bd.adamw_values(s["v"], True), "ms": s["ms"], "vs": s["vs"]}
+    return {"p": s["p"], "p16": s["p16"], **states}
 
 
 def run(state):
