@@ -492,14 +492,15 @@ bd_status bd_lora_multitenant_backward(const uint16_t* dy_f16, const uint16_t* x
  * multiply by) or whole matrices (whose fp16 copy bd_compress takes).  Per element, in binary32:
  *     g = grad * grad_scale;   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g g
  *     p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps);   p_f16 = fp16(p)
- * A PLAN holds the tensors' addresses and sizes, checked once: a block of bytes in HOST memory (8-byte aligned) that the caller
- * owns and may copy; bd_adamw reads it while it enqueues and keeps nothing of it.
+ * A PLAN holds the tensors' addresses and sizes, checked once: bd_adamw_plan_bytes(n, numel) bytes in HOST memory (8-byte aligned)
+ * that the caller owns.  A step reads it, and the kernels a copy of the same bytes in DEVICE memory (16-byte aligned) that the caller
+ * makes once; all tensors are one launch.
  *   n                       tensors, up to BD_ADAMW_MAX_TENSORS; entries of HOST arrays of n DEVICE pointers below
  *   param                   binary32, updated in place;  param_f16: their fp16 copies, written; the array or entries may be NULL
  *   grad                    binary32, or fp16 where grad_f16 != 0
  *   exp_avg, exp_avg_sq     m and v: binary32, or one byte per element where the two scale arrays are given
  *   exp_avg_scale, exp_avg_sq_scale   NULL, or one float per block of 256 elements of a tensor (its last block may be shorter)
- *   numel                   HOST [n], 0 .. BD_ADAMW_MAX_ELEMENTS; a tensor of none is skipped
+ *   numel                   HOST [n], 0 .. BD_ADAMW_MAX_ELEMENTS; a tensor of none is skipped (bytes 0: too many together)
  * Tensors 16-byte aligned, scales 4.  Nothing may overlap anything else (BD_ERR_ALIAS): no tensor twice.
  * States in 8 bits: a byte's value is V times its block's scale, V = f where the exponent bits e are 0, else (2^F + f) 2^(e-1).
  *     m: bit 7 the sign, bits 6-4 e, bits 3-0 f (F = 4); m = +-scale V, rounded to nearest even; scale = max |m| / 1984
@@ -508,20 +509,23 @@ bd_status bd_lora_multitenant_backward(const uint16_t* dy_f16, const uint16_t* x
  *   The update itself uses m and v before they are rounded.  All zeros (bytes and scales) is the state before the first step.  A
  *   block with an infinity or NaN becomes NaN; one whose largest |m| is below 2^-100 becomes zero.
  * bd_adamw:
+ *   plan_device             the copy of the plan's bytes on the device
  *   lr, step                device, one float and one int64: the learning rate and the number t >= 1 of this step (read when
  *                           the kernel runs, so that a captured step can be replayed with the next ones)
  *   grad_scale              device, one float, or NULL (1): what undoes a loss scale, or clips
  *   skip                    device, one int32, or NULL: not 0 leaves everything as it was (a step whose gradients overflowed)
  *   beta1, beta2 in [0, 1), eps, weight_decay >= 0, else BD_ERR_UNSUPPORTED.  BD_ERR_FORMAT: not a plan.
- * 40 tensors per launch. */
+ * bd_adamw_values: the values V (with m's sign) of 8-bit states in fp16, which holds them exactly: values_f16 [n] from codes [n],
+ *   second == 0: of m, else of v; 16-byte aligned.  To read states out: m = V scale, sqrt(v) = V scale. */
 #define BD_ADAMW_MAX_TENSORS 1048576
 #define BD_ADAMW_MAX_ELEMENTS ((int64_t)1 << 35)
-size_t bd_adamw_plan_bytes(int32_t n);
+size_t bd_adamw_plan_bytes(int32_t n, const int64_t* numel);
 bd_status bd_adamw_plan(void* plan, size_t plan_bytes, int32_t n, float* const* param, uint16_t* const* param_f16, const void* const* grad,
                         int32_t grad_f16, void* const* exp_avg, void* const* exp_avg_sq, float* const* exp_avg_scale,
                         float* const* exp_avg_sq_scale, const int64_t* numel);
-bd_status bd_adamw(const void* plan, size_t plan_bytes, const float* lr, const int64_t* step, const float* grad_scale, const int32_t* skip,
-                   double beta1, double beta2, double eps, double weight_decay, void* stream);
+bd_status bd_adamw(const void* plan, size_t plan_bytes, const void* plan_device, const float* lr, const int64_t* step, const float* grad_scale,
+                   const int32_t* skip, double beta1, double beta2, double eps, double weight_decay, void* stream);
+bd_status bd_adamw_values(const uint8_t* codes, int64_t n, int32_t second, uint16_t* values_f16, void* stream);
 
 /* ---- delta images: storing a tenant's delta and swapping it in while serving ----------------
  * Sec. 3.3 of the paper: a 1-bit delta is small enough to be kept per tenant on disk or in host

@@ -35,7 +35,8 @@ EXPORTS = ["bd_status_string", "bd_version", "bd_workspace_bytes", "bd_pack_sign
            "bd_linear_multitenant_tiled_group_q8", "bd_linear_multitenant_kbit", "bd_linear_multitenant_gemm_kbit",
            "bd_linear_multitenant_gemm_q8", "bd_linear_multitenant_q8", "bd_linear_multitenant_gemm_kbit_variant",
            "bd_linear_multitenant_gemm_q8_variant", "bd_lora_workspace_bytes", "bd_lora_multitenant", "bd_lora_multitenant_group",
-           "bd_lora_backward_workspace_bytes", "bd_lora_multitenant_backward", "bd_adamw_plan_bytes", "bd_adamw_plan", "bd_adamw"]
+           "bd_lora_backward_workspace_bytes", "bd_lora_multitenant_backward", "bd_adamw_plan_bytes", "bd_adamw_plan", "bd_adamw",
+           "bd_adamw_values"]
 
 
 class BitDeltaError(RuntimeError):
@@ -125,10 +126,11 @@ def lib() -> ctypes.CDLL:
         L.bd_lora_backward_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
         L.bd_lora_multitenant_backward.argtypes = [vp, vp, vp, i32, pvp, pvp, pi, vp, vp, vp, vp, pvp, pvp, i32, i64, i64, i64, i32, vp, sz, vp]
         L.bd_adamw_plan_bytes.restype = sz
-        L.bd_adamw_plan_bytes.argtypes = [i32]
+        L.bd_adamw_plan_bytes.argtypes = [i32, pi64]
         L.bd_adamw_plan.argtypes = [vp, sz, i32, pvp, pvp, pvp, i32, pvp, pvp, pvp, pvp, pi64]
         dbl = ctypes.c_double
-        L.bd_adamw.argtypes = [vp, sz, vp, vp, vp, vp, dbl, dbl, dbl, dbl, vp]
+        L.bd_adamw.argtypes = [vp, sz, vp, vp, vp, vp, vp, dbl, dbl, dbl, dbl, vp]
+        L.bd_adamw_values.argtypes = [vp, i64, i32, vp, vp]
         for name in ("bd_pack_signs", "bd_compress", "bd_linear_multitenant", "bd_linear_multitenant_variant",
                      "bd_materialize", "bd_linear_naive", "bd_probe_read", "bd_probe_copy", "bd_tile_base",
                      "bd_tile_signs", "bd_linear_multitenant_tiled", "bd_linear_multitenant_tiled_group"):
@@ -878,9 +880,9 @@ LORA_MAX_RANK = 256
 
 def _here(*tensors) -> None:
     """The tensors of a call are on the current device: its kernels run there."""
-    dev = torch.cuda.current_device()
+    dev = torch.cuda.current_device() if _current_device is None or not torch.cuda.is_initialized() else _current_device()
     for t in tensors:
-        if t is not None and t.device.index != dev:
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
 
 
@@ -1130,11 +1132,12 @@ class AdamWGroup:
         self.keep, self.n = lists, n
         ptrs = lambda ts: (ctypes.c_void_p * max(n, 1))(*[_ptr(t) or None for t in ts])
         numel = (ctypes.c_int64 * max(n, 1))(*[int(p.numel()) for p in lists[0]])
-        self.bytes = int(lib().bd_adamw_plan_bytes(n))
+        self.bytes = int(lib().bd_adamw_plan_bytes(n, numel))
         self.plan = (ctypes.c_uint64 * max((self.bytes + 7) // 8, 1))()
         _check(lib().bd_adamw_plan(self.plan, self.bytes, n, ptrs(lists[0]), ptrs(lists[4]), ptrs(lists[1]), int(grad_type == torch.float16),
                                    ptrs(lists[2]), ptrs(lists[3]), ptrs(lists[5]) if bits8 else None, ptrs(lists[6]) if bits8 else None,
                                    numel), "bd_adamw_plan")
+        self.plan_device = torch.frombuffer(self.plan, dtype=torch.uint8).to(self.device) if n else None
 
 
 def adamw(group: AdamWGroup, lr: torch.Tensor, step: torch.Tensor, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
@@ -1147,5 +1150,18 @@ def adamw(group: AdamWGroup, lr: torch.Tensor, step: torch.Tensor, beta1: float 
             raise ValueError(f"{what} is one number")
     if group.n:
         _here(lr, step, grad_scale, skip, group.keep[0][0])
-    _check(lib().bd_adamw(group.plan, group.bytes, _ptr(lr), _ptr(step), _ptr(grad_scale), _ptr(skip), beta1, beta2, eps, weight_decay,
+    _check(lib().bd_adamw(group.plan, group.bytes, _ptr(group.plan_device), _ptr(lr), _ptr(step), _ptr(grad_scale), _ptr(skip), beta1, beta2, eps, weight_decay,
                           _stream(stream)), "bd_adamw")
+
+
+def adamw_values(codes: torch.Tensor, second: bool, values: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """bd_adamw_values: what the bytes of 8-bit states stand for, in units of their blocks' scales (second: of sqrt(v), else of m with its
+    sign), as float16, which holds the values exactly."""
+    _dev(codes, torch.uint8, "codes")
+    if values is None:
+        values = torch.empty(codes.shape, dtype=torch.float16, device=codes.device)
+    if _dev(values, torch.float16, "values").numel() != codes.numel():
+        raise ValueError("one value per code")
+    _here(codes, values)
+    _check(lib().bd_adamw_values(_ptr(codes), codes.numel(), int(second), _ptr(values), _stream(stream)), "bd_adamw_values")
+    return values

@@ -903,7 +903,7 @@ constexpr int kGradPitch = 128 + 16;   // halves: 4 rows apart on banks of their
 // is 2^-64 of the largest so far are below what binary32 would keep of them.
 // Loads are never under a condition (past the end they repeat the last tile's), or the wait for them would be for all.
 template <int RW, bool ODD>
-__global__ __launch_bounds__(kGradThreads, ODD ? 2 : 3) void lora_grad_kernel(const LoraGradArgs a) {
+__global__ __launch_bounds__(kGradThreads, RW == 1 && !ODD ? 3 : 1) void lora_grad_kernel(const LoraGradArgs a) {
     constexpr int TW = kLoraGradWaves / RW, N = 8 / RW, kBuffers = RW > 1 ? 2 : 1;   // groups; rows of 4 per wavefront and tile
     typedef _Float16 Tile[32][kGradPitch];
     constexpr size_t kTiles = sizeof(Tile) * TW * kBuffers, kSums = sizeof(float) * kLoraGradWaves * 8 * 4 * kWave;

@@ -133,7 +133,7 @@ def test_step(bits, grad, step, scaled):
         assert ((got - u).abs() <= cell * (1 + 1e-3)).all()
 
 
-def test_many_tensors_take_several_launches():
+def test_many_tensors():
     sizes = [(37 * i) % 900 + 1 for i in range(131)]
     for bits in (32, 8):
         prob = Problem(sizes, bits, "f32", seed=5, copies=False)
@@ -248,3 +248,14 @@ def test_replayed_from_a_graph():
             torch.cuda.synchronize()
             for u, w in zip(prob.p + prob.p16 + prob.m + prob.v, eager.p + eager.p16 + eager.m + eager.v):
                 assert u is None or torch.equal(u, w), f"replay {rep}"
+
+
+def test_values_of_codes():
+    """Every code, both states, and lengths that are not whole."""
+    codes = torch.arange(256, dtype=torch.int32).to(torch.uint8).to(DEV)
+    assert torch.equal(bd.adamw_values(codes, False).cpu().double(), M_VALUES) and torch.equal(bd.adamw_values(codes, True).cpu().double(), V_VALUES)
+    for n in (1, 7, 8, 9, 2049, 100003):
+        c = torch.randint(0, 256, (n,), dtype=torch.uint8, device=DEV)
+        for second, table in ((False, M_VALUES), (True, V_VALUES)):
+            assert torch.equal(bd.adamw_values(c, second).cpu().double(), table[c.cpu().long()]), n
+    assert bd.adamw_values(codes[:0], True).numel() == 0

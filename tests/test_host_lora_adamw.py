@@ -112,12 +112,13 @@ def test_backward_argument_errors(bd):
 
 def test_adamw_argument_errors(bd):
     L = bd.lib()
-    n = 2
-    nbytes = L.bd_adamw_plan_bytes(n)
-    assert nbytes > L.bd_adamw_plan_bytes(1) > L.bd_adamw_plan_bytes(0) > 0
-    assert L.bd_adamw_plan_bytes(-1) == 0 and L.bd_adamw_plan_bytes(1048577) == 0
+    numel = lambda *v: (ctypes.c_int64 * max(len(v), 1))(*v)
+    size_of = L.bd_adamw_plan_bytes
+    nbytes = size_of(2, numel(300, 7))
+    assert size_of(2, numel(30000, 7)) > nbytes > size_of(1, numel(300)) > size_of(0, None) > 0
+    assert size_of(-1, None) == 0 and size_of(1048577, None) == 0 and size_of(1, None) == 0
+    assert size_of(1, numel(-1)) == 0 and size_of(1, numel((1 << 35) + 1)) == 0 and size_of(200, numel(*([1 << 35] * 200))) == 0
     plan = (ctypes.c_uint64 * (nbytes // 8 + 1))()
-    numel = lambda *v: (ctypes.c_int64 * len(v))(*v)
 
     def make(to=plan, size=nbytes, n=2, p=_ptrs(A, 2 * A), p16=_ptrs(3 * A, None), g=_ptrs(4 * A, 5 * A), m=_ptrs(6 * A, 7 * A), v=_ptrs(8 * A, 9 * A),
              ms=_ptrs(10 * A, 11 * A), vs=_ptrs(12 * A, 13 * A), count=numel(300, 7)):
@@ -136,11 +137,11 @@ def test_adamw_argument_errors(bd):
     assert make(g=_ptrs(4 * A, 4 * A)) == 0                                                 # read twice is no overlap
     assert make(p=_ptrs(None, 2 * A), g=_ptrs(None, 5 * A), count=numel(0, 7)) == 0         # nothing of an empty tensor is looked at
 
-    step = lambda p=plan, size=nbytes, lr=14 * A, t=15 * A, gs=0, skip=0, b1=0.9, b2=0.999, eps=1e-8, wd=0.0: L.bd_adamw(p, size, lr, t, gs, skip, b1, b2, eps, wd, 0)
+    step = lambda p=plan, size=nbytes, dev=16 * A, lr=14 * A, t=15 * A, gs=0, skip=0, b1=0.9, b2=0.999, eps=1e-8, wd=0.0: L.bd_adamw(p, size, dev, lr, t, gs, skip, b1, b2, eps, wd, 0)
     assert make() == 0
-    assert step(p=None) == 1 and step(lr=0) == 1 and step(t=0) == 1
+    assert step(p=None) == 1 and step(dev=0) == 1 and step(dev=16 * A + 8) == 3 and step(lr=0) == 1 and step(t=0) == 1
     assert step(lr=14 * A + 2) == 3 and step(t=15 * A + 4) == 3 and step(gs=A + 1) == 3 and step(skip=A + 2) == 3
-    assert step(size=8) == 9 and step(size=nbytes - 1) == 9
+    assert step(size=8) == 9 and step(size=nbytes - 8) == 9
     junk = (ctypes.c_uint64 * 64)(*([7] * 64))
     assert step(p=junk, size=512) == 9
     nan = float("nan")
@@ -169,3 +170,10 @@ def test_binding_refusals(bd):
         bd._tok_pointer(torch.zeros(3, dtype=torch.int64), 3)
     with pytest.raises(ValueError):
         bd._tok_pointer([0, 1], 3)
+
+
+def test_adamw_values_argument_errors(bd):
+    f = bd.lib().bd_adamw_values
+    assert f(A, -1, 0, 2 * A, 0) == 2 and f(A, (1 << 35) + 1, 0, 2 * A, 0) == 2
+    assert f(0, 8, 0, 2 * A, 0) == 1 and f(A, 8, 0, 0, 0) == 1 and f(A + 8, 8, 0, 2 * A, 0) == 3 and f(A, 8, 0, 2 * A + 8, 0) == 3
+    assert f(A, 64, 0, A + 32, 0) == 8 and f(0, 0, 0, 0, 0) == 0
