@@ -112,13 +112,13 @@ struct LoraPrepArgs {
 };
 
 // side 0: dA [r][F] = sum over a job's tokens of g[token][r] x[token][f];  side 1: dB [F][r] = scale * sum of dy[token][f] h[token][r]
-constexpr int kLoraGradJobs = 52;
+constexpr int kLoraGradJobs = 48;
 constexpr int kLoraPartTokens = 4096;   // most tokens of a part
 constexpr int lora_grad_rank_waves(int max_rank) { return max_rank <= 16 ? 1 : max_rank <= 32 ? 2 : 4; }   // wavefronts that share a tile
 struct LoraGradJob {
     float* out[2];                      // nullptr: not wanted
     int32_t partial;                    // where its parts begin in `partial`, in rows of F
-    int32_t tenant, count, first, rank, chunk_begin, parts;
+    int32_t tenant, count, first, rank, chunk_begin, parts, part_chunks;   // part_chunks: chunks of 32 tokens of each part but the last
 };
 struct LoraGradSide {
     const uint16_t* d;                  // [T, F]

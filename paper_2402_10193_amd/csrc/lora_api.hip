@@ -305,12 +305,12 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
 
 // Parts of every job's tokens in the gradients' sums: one, or more where that fills the compute units better (the parts must then be
 // added up).  A workgroup of RW wavefronts to a tile takes some 5 us and 0.35 us for every tile of 32 tokens that each of its 4 / RW groups
-// takes; 3 or 4 run on a compute unit at a time.
+// takes; 3 run on a compute unit at a time.
 void cut_into_parts(bd::LoraGradJob* job, int n, int64_t wide, int rank, int64_t most) {
     int longest = 1;
     for (int i = 0; i < n; ++i) longest = std::max(longest, (int)job[i].count);
     const int RW = bd::lora_grad_rank_waves(rank), TW = bd::kLoraGradWaves / RW;
-    const int64_t slots = (int64_t)compute_units() * (RW == 1 ? 3 : 4);
+    const int64_t slots = (int64_t)compute_units() * 3;
     int best = std::min(longest, bd::kLoraPartTokens);
     double least = 1e30;
     for (int cut = 1; cut <= kGradParts; ++cut) {
@@ -326,7 +326,11 @@ void cut_into_parts(bd::LoraGradJob* job, int n, int64_t wide, int rank, int64_t
         const double us = (double)rounds * (5.0 + 0.35 * (double)((tokens + 32 * TW - 1) / (32 * TW))) + (partial ? 4.0 + (double)partial * rank * wide * 128 * 8 / 3e6 : 0.0);
         if (us < least) least = us, best = tokens;
     }
-    for (int i = 0; i < n; ++i) job[i].parts = (job[i].count + best - 1) / best;
+    for (int i = 0; i < n; ++i) {
+        job[i].parts = (job[i].count + best - 1) / best;
+        job[i].part_chunks = ((job[i].count + 31) / 32 + job[i].parts - 1) / job[i].parts;
+        job[i].parts = ((job[i].count + 31) / 32 + job[i].part_chunks - 1) / job[i].part_chunks;   // (no part without tokens)
+    }
 }
 
 bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_t h_ld, const uint16_t* const* a_by, const uint16_t* const* b_by,
@@ -470,7 +474,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
                 const int rank = rank_by[j.tenant];
                 prep->job[i] = bd::LoraPrepJob{j.first, j.count, rank, chunk};
                 args->job[i] = bd::LoraGradJob{{da_by && in > 0 ? da_by[j.tenant] : nullptr, db_by && out > 0 ? db_by[j.tenant] : nullptr},
-                                               0, j.tenant, j.count, j.first, rank, chunk, 1};
+                                               0, j.tenant, j.count, j.first, rank, chunk, 1, 0};
                 chunk += (j.count + 31) / 32;
                 most = std::max(most, rank);
             }

@@ -328,14 +328,14 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
     // Steps of 32 elements.  A last one of fewer (the backward pass's only: K is then `out`) is the last 32 elements, those zero that
     // an earlier step has had; a K below 32 is read element by element.
     // The wavefronts of a workgroup take neighbouring steps, so that what it reads of a row at a time is a run of 256 bytes.
-    const int64_t parts = (int64_t)a.splits * kLoraShrinkWaves, part = (int64_t)blockIdx.y * kLoraShrinkWaves + wave;
-    const int64_t whole = a.K / 32, mine = part < whole ? (whole - part + parts - 1) / parts : 0;   // steps part, part + parts, ...
+    const int parts = a.splits * kLoraShrinkWaves, part = (int)blockIdx.y * kLoraShrinkWaves + wave;
+    const int whole = (int)(a.K / 32), mine = part < whole ? (int)((unsigned)(whole - part + parts - 1) / (unsigned)parts) : 0;   // steps part, part + parts, ...
     constexpr int C = ODD ? 1 : NT * RT == 1 ? 4 : NT + RT <= 5 ? 2 : 1;   // steps of one of two buffers: what the registers hold
     half8 xv[2][C][NT], wv[2][C][RT];
-    auto load = [&](int buffer, int64_t s) {   // (a step beyond the last repeats it)
+    auto load = [&](int buffer, int s) {   // (a step beyond the last repeats it)
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int64_t k0 = 32 * (part + parts * min(s + c, mine - 1));
+            const int64_t k0 = 32 * (part + (int64_t)parts * min(s + c, mine - 1));
 #pragma unroll
             for (int n = 0; n < NT; ++n) xv[buffer][c][n] = load8(row[n] + k0);
 #pragma unroll
@@ -386,19 +386,19 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
     // Two buffers; loads are never under a condition (past the end they repeat the last step's), or the wait for them would be for all.
     if (mine > 0) {
         load(0, 0);
-        int64_t s = 0;
+        int s = 0;
         for (; s + 2 * C <= mine; s += 2 * C) {
             load(1, s + C);
 #pragma unroll
-            for (int c = 0; c < C; ++c) product(xv[0][c], wv[0][c], 32 * (part + parts * (s + c)), 0, 32);
+            for (int c = 0; c < C; ++c) product(xv[0][c], wv[0][c], 32 * (part + (int64_t)parts * (s + c)), 0, 32);
             load(0, s + 2 * C);
 #pragma unroll
-            for (int c = 0; c < C; ++c) product(xv[1][c], wv[1][c], 32 * (part + parts * (s + C + c)), 0, 32);
+            for (int c = 0; c < C; ++c) product(xv[1][c], wv[1][c], 32 * (part + (int64_t)parts * (s + C + c)), 0, 32);
         }
         if (C > 1) load(1, s + C);
 #pragma unroll
         for (int c = 0; c < 2 * C - 1; ++c)
-            if (s + c < mine) product(xv[c / C][c % C], wv[c / C][c % C], 32 * (part + parts * (s + c)), 0, 32);
+            if (s + c < mine) product(xv[c / C][c % C], wv[c / C][c % C], 32 * (part + (int64_t)parts * (s + c)), 0, 32);
     }
     if constexpr (TR) {
         if (a.K % 32 != 0 && whole % parts == part) {   // the last step, of fewer than 32
@@ -468,6 +468,7 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
     // read element by element
     const int64_t f0 = ((int64_t)blockIdx.y * kLoraExpandWaves + wave) * kLoraFeatures, base = min(f0, max(F - kLoraFeatures, (int64_t)0)), f = base + 8 * m;
     const bool active = f0 < F, vectors = !ODD || F >= kLoraFeatures;
+    const float scale = TR || u.rank == 0 ? 1.0f : a.scale[u.mat][u.tenant];
 
     int64_t at[4];   // where the lane's results belong: token 4 g + i
     half8 before[4];
@@ -545,7 +546,7 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
 #pragma unroll
     for (int d = kPer / 2; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
     const int e = group_exponent(top);
-    if (sub == 0) unit[c] = power_of_two(e) * (TR || u.rank == 0 ? 1.0f : a.scale[u.mat][u.tenant]);
+    if (sub == 0) unit[c] = power_of_two(e) * scale;
     const float down = power_of_two(-e);
     for (int r = 4 * sub; r < padded; r += 4 * kPer) {
         const float4v v = r == 4 * sub ? first : sum4(r);
@@ -655,6 +656,7 @@ __global__ __launch_bounds__(kExpandThreads, ODD ? 2 : 3) void lora_expand_many_
     // Features f0 .. f0 + 127; a row's last 128 end with it, and of them only those from f0 on are kept.  A row below 128 is read element
     // by element.
     int64_t f0 = (int64_t)blockIdx.y * kLoraFeatures;
+    const float scale = TR || u.rank == 0 ? 1.0f : a.scale[u.mat][u.tenant];
     const bool vectors = !ODD || F >= kLoraFeatures;
     auto begin_of = [&](int64_t first) { return min(first, max(F - kLoraFeatures, (int64_t)0)); };
 
@@ -745,7 +747,7 @@ __global__ __launch_bounds__(kExpandThreads, ODD ? 2 : 3) void lora_expand_many_
 #pragma unroll
     for (int d = kPer / 2; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
     const int e = group_exponent(top);
-    if (sub == 0) unit[c] = power_of_two(e) * (TR || u.rank == 0 ? 1.0f : a.scale[u.mat][u.tenant]);
+    if (sub == 0) unit[c] = power_of_two(e) * scale;
     const float down = power_of_two(-e);
     for (int r = 4 * sub; r < padded; r += 4 * kPer) {
         const float4v v = r == 4 * sub ? first : sum4(r);
@@ -903,13 +905,13 @@ constexpr int kGradPitch = 128 + 16;   // halves: 4 rows apart on banks of their
 // is 2^-64 of the largest so far are below what binary32 would keep of them.
 // Loads are never under a condition (past the end they repeat the last tile's), or the wait for them would be for all.
 template <int RW, bool ODD>
-__global__ __launch_bounds__(kGradThreads, RW == 1 && !ODD ? 3 : 1) void lora_grad_kernel(const LoraGradArgs a) {
+__global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(ODD ? 2 : 3, 3))) void lora_grad_kernel(const LoraGradArgs a) {
     constexpr int TW = kLoraGradWaves / RW, N = 8 / RW, kBuffers = RW > 1 ? 2 : 1;   // groups; rows of 4 per wavefront and tile
     typedef _Float16 Tile[32][kGradPitch];
     constexpr size_t kTiles = sizeof(Tile) * TW * kBuffers, kSums = sizeof(float) * kLoraGradWaves * 8 * 4 * kWave;
     __shared__ __align__(16) char lds[kTiles > kSums ? kTiles : kSums];
     __shared__ uint16_t ids[kLoraPartTokens];
-    const int which = (int)blockIdx.z / a.rank_groups, rt0 = (int)blockIdx.z % a.rank_groups * RW;
+    const int which = (int)blockIdx.z >= a.rank_groups ? 1 : 0, rt0 = ((int)blockIdx.z - which * a.rank_groups) * RW;
     const LoraGradSide& side = a.side[which];
     int which_job = 0;
 #pragma unroll
@@ -922,8 +924,8 @@ __global__ __launch_bounds__(kGradThreads, RW == 1 && !ODD ? 3 : 1) void lora_gr
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, group = wave / RW, rank_wave = wave % RW;
     const int n = lane & 15, q = lane >> 4;
     // the part's tokens, t0 .. t0 + count - 1 of the job; whole tiles of 32 but for the job's last
-    const int chunks_all = (job.count + 31) / 32, c0 = (int)((int64_t)chunks_all * split / job.parts), c1 = (int)((int64_t)chunks_all * (split + 1) / job.parts);
-    const int t0 = 32 * c0, count = min(32 * c1, job.count) - t0, chunks = c1 - c0;
+    const int c0 = split * job.part_chunks, t0 = 32 * c0, count = min(32 * job.part_chunks, job.count - t0), chunks = (count + 31) / 32;
+    const float scale = side.scale ? side.scale[job.tenant] : 1.0f;
     for (int i = threadIdx.x; i < 32 * chunks; i += kGradThreads) {   // (behind the last token: the first once more)
         const int p = job.first + t0 + (i < count ? i : 0);
         ids[i] = (uint16_t)(a.order ? a.order[p] : p);
@@ -1011,7 +1013,6 @@ __global__ __launch_bounds__(kGradThreads, RW == 1 && !ODD ? 3 : 1) void lora_gr
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[wave][j][i][lane] = acc[j][i] * up;
     __syncthreads();
-    const float scale = side.scale ? side.scale[job.tenant] : 1.0f;
     float* const out = job.parts > 1 ? side.partial + (job.partial + (int64_t)split * rank_all) * F : result;
     const bool add = a.accumulate && job.parts == 1;
     constexpr int kRanks = 16 * RW;
