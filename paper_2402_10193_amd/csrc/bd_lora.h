@@ -29,13 +29,14 @@ struct LoraTile {                       // few tokens
     uint16_t rank, count, mat, unused;
     uint32_t col[8];                    // the tokens, two per word
 };
-struct LoraDecodeTile {                 // a few tokens of a tenant, low ranks: both products in one launch
+struct LoraDecodeTile {                 // one or two tokens of a tenant, low ranks: both products in one launch
     const uint16_t *wa, *wb;
     int32_t tenant;
     uint16_t rank, count, mat, unused;
-    uint16_t col[4];
+    uint16_t col[2];
 };
-constexpr int kLoraDecodeTokens = 4, kLoraDecodeRank = 32;   // at most, of such a tile
+constexpr int kLoraDecodeTokens = 2, kLoraDecodeRank = 16;   // at most, of such a tile
+constexpr int kLoraDecodeRecords = 112;                      // of a launch: with the rest below the 4 KB of a kernel's arguments
 constexpr int kLoraDecodeFeatures = 1024;                    // of a workgroup
 
 struct LoraJob {                        // many tokens
@@ -91,7 +92,7 @@ struct LoraDecodeArgs {
     int64_t F[kLoraMaxMats];
     int64_t in;
     int32_t n_tiles, h_ld;
-    LoraDecodeTile tile[kLoraRecords];
+    LoraDecodeTile tile[kLoraDecodeRecords];
 };
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));

@@ -16,7 +16,7 @@ using bd::overlaps;
 
 constexpr int kFewColumns = 16, kManyColumns = bd::kLoraExpandTokens;   // tokens of a tile: records are tiles, or jobs
 constexpr int64_t kFewTokens = 512;                  // largest batch whose records are tiles
-constexpr int64_t kDecodeBytes = 256 << 10;          // of A, that every workgroup of a decode launch reads
+constexpr int64_t kDecodeIn = 12288, kDecodeWeight = (int64_t)1 << 28;   // most of in x tokens, of in x out, of a decode launch
 constexpr int kGradParts = 32;                       // parts of jobs whose tokens are in more than one, of all jobs together
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
@@ -141,12 +141,15 @@ bool sizes_ok(int64_t T, int64_t out, int64_t in, int32_t n_tenants) {
     return T >= 0 && T <= 65535 && out >= 0 && in >= 0 && n_tenants >= 0 && in % 32 == 0 && out <= (int64_t)1 << 24 && in <= (int64_t)1 << 24;
 }
 
-// Both products in one launch (lora_decode_kernel), where it is quicker: a few tokens of every tenant, low ranks, and an A that every workgroup
-// can read again: TODO measured.
-bool decode_fits(const Batch& b, int max_rank, int64_t in) {
-    if (max_rank > bd::kLoraDecodeRank || in < 8 || (int64_t)max_rank * in * 2 > kDecodeBytes) return false;
+// Both products in one launch (lora_decode_kernel), where it is quicker than two.  Every workgroup reads all of A and multiplies it with
+// each of its tenant's tokens, so its time grows with in x tokens, and with in x out where many tenants' workgroups share the caches.
+// Rank 16, out = 4096, 16 tenants, one launch against two: in = 4096: 5.0 / 7.9 us, 2 tokens each 7.0 / 7.8, 4 each 10.7 / 8.1;
+// in = 11008: 7.8 / 8.2, 2 each 11.8 / 8.1; in = 28672: 13.3 / 9.6.  64 tenants, out = 32000: in = 4096: 25.1 / 34.7, 8192: 35.6 / 37.0,
+// 11008: 47.8 / 37.9.  Rank 32 has each of its wavefronts read twice as many rows: in = 4096, 64 tenants: 12.8 / 11.3.
+bool decode_fits(const Batch& b, int max_rank, int64_t in, int64_t max_out) {
+    if (max_rank > bd::kLoraDecodeRank || in < 8 || in * max_out > kDecodeWeight) return false;
     for (const Job& j : b.jobs)
-        if (j.count > bd::kLoraDecodeTokens) return false;
+        if (j.count > bd::kLoraDecodeTokens || in * j.count > kDecodeIn) return false;
     return true;
 }
 
@@ -209,7 +212,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
     // without an adapter there is nothing to do where y is y0
     auto takes_part = [&](int m, int32_t rank) { return (out[m] > 0 || (h && h[m])) && (rank > 0 || !(y0 && y0[m] == y[m])); };
     // ---- checked: launches from here on ----
-    if (decode_fits(batch, max_rank, in)) {
+    if (decode_fits(batch, max_rank, in, max_out)) {
         auto d = std::make_unique<bd::LoraDecodeArgs>();
         for (int m = 0; m < n_mats; ++m) {
             d->y0[m] = y0 ? y0[m] : nullptr;
@@ -235,11 +238,11 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
                 const size_t at = (size_t)m * n_tenants + j.tenant;
                 if (!takes_part(m, rank_by[at])) continue;
                 bd::LoraDecodeTile& t = d->tile[d->n_tiles++];
-                t = bd::LoraDecodeTile{a_by[at], b_by[at], j.tenant, (uint16_t)rank_by[at], (uint16_t)j.count, (uint16_t)m, 0, {0, 0, 0, 0}};
+                t = bd::LoraDecodeTile{a_by[at], b_by[at], j.tenant, (uint16_t)rank_by[at], (uint16_t)j.count, (uint16_t)m, 0, {0, 0}};
                 for (int c = 0; c < j.count; ++c) t.col[c] = (uint16_t)batch.token(j.first + c);
                 tokens = std::max(tokens, (int)j.count);
                 odd |= rank_by[at] % 8 != 0;
-                if (d->n_tiles == bd::kLoraRecords && !flush()) return BD_ERR_DEVICE;
+                if (d->n_tiles == bd::kLoraDecodeRecords && !flush()) return BD_ERR_DEVICE;
             }
         return flush() ? BD_OK : BD_ERR_DEVICE;
     }

@@ -133,7 +133,7 @@ __device__ __forceinline__ void tokens_of(const Args& a, const Where& u, const i
 
 constexpr int kDecodeThreads = 512;
 
-// A decode step: up to 4 tokens of a tenant, up to 32 ranks, both products in one launch, bound by latency.  Every workgroup of 1024
+// A decode step: up to 2 tokens of a tenant, up to 16 ranks, both products in one launch, bound by latency.  Every workgroup of 1024
 // features forms all of h (A comes out of the cache again for the next one): a launch and the way of h through memory would take longer.
 // Vector arithmetic: a wavefront reads rows of A as they are, 1 KB of a row per instruction, and a lane the rows of B of its two features;
 // the matrix cores' order would take the address unit four times as long.  y0 and B are asked for before h is formed.
@@ -1053,8 +1053,8 @@ hipError_t launch_lora_decode(const LoraDecodeArgs& a, int max_tokens, int64_t m
         hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)groups), dim3(kDecodeThreads), 0, st, a);
         return hipGetLastError();
     };
-    if (odd) return max_tokens == 1 ? go(lora_decode_kernel<1, true>) : max_tokens == 2 ? go(lora_decode_kernel<2, true>) : go(lora_decode_kernel<4, true>);
-    return max_tokens == 1 ? go(lora_decode_kernel<1, false>) : max_tokens == 2 ? go(lora_decode_kernel<2, false>) : go(lora_decode_kernel<4, false>);
+    if (odd) return max_tokens == 1 ? go(lora_decode_kernel<1, true>) : go(lora_decode_kernel<2, true>);
+    return max_tokens == 1 ? go(lora_decode_kernel<1, false>) : go(lora_decode_kernel<2, false>);
 }
 
 hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transposed, int max_rank, bool odd, hipStream_t st) {
