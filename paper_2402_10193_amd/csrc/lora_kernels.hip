@@ -35,6 +35,15 @@ __device__ __forceinline__ half8 load8_each(const uint16_t* p, int64_t last) {
     for (int i = 0; i < 8; ++i) v[i] = *(const _Float16*)(p + (i < last ? i : last));
     return v;
 }
+// Elements at .. at + 7 of an array of n, those behind its end anything: the last 8, moved.  Rows that do not begin at 16 bytes, read past
+// their ends.
+template <bool SHORT>   // n may be below 8
+__device__ __forceinline__ half8 load8_of(const uint16_t* p, int64_t at, int64_t n) {
+    if (SHORT && n < 8) return load8_each(p + min(at, n - 1), max(n - 1 - at, (int64_t)0));
+    const int64_t from = min(at, n - 8);
+    const half8 v = load8(p + from);
+    return __builtin_bit_cast(half8, __builtin_bit_cast(unsigned __int128, v) >> (16 * (int)min(at - from, (int64_t)7)));
+}
 // v with zeros where element i is not in [first, end)
 __device__ __forceinline__ half8 only(half8 v, int first, int end) {
 #pragma unroll
@@ -441,6 +450,8 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
 }
 
 constexpr int kExpandThreads = kLoraExpandWaves * kWave;
+// Kernels of their own for the rows of the weights and results: 16-byte pieces, ranks that are no multiple of 8, fewer than 128 features
+enum { kEvenRanks, kOddRanks, kShortRows };
 
 // Few tokens: y = y0 + s B h, or dx = dx0 + A^T g, of one tile of 16 tokens by 512 features, 128 for each wavefront.  h comes in as
 // `splits` partial sums.  Rows of a result are tokens, columns features: feature 8 n + j of a wavefront's 128 is column n of its MFMA
@@ -451,7 +462,7 @@ constexpr int kExpandThreads = kLoraExpandWaves * kWave;
 // 8 ranks' rows of A are turned in registers.
 // y0 and the first weights are asked for before h is prepared: three waits for memory become one.
 constexpr int kFewStage = 128 * 64 + 16 * 16;   // bytes
-template <bool TR, bool ODD>
+template <bool TR, int ROWS>
 __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const LoraExpandArgs a) {
     constexpr int kTokens = 16, kPer = kExpandThreads / kTokens;   // threads per token while h is prepared
     extern __shared__ __align__(16) char lds[];
@@ -467,7 +478,7 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
     // the wavefront's features, f0 .. f0 + 127; the last one's 128 end with the row and it keeps what is its own; a row below 128 is
     // read element by element
     const int64_t f0 = ((int64_t)blockIdx.y * kLoraExpandWaves + wave) * kLoraFeatures, base = min(f0, max(F - kLoraFeatures, (int64_t)0)), f = base + 8 * m;
-    const bool active = f0 < F, vectors = !ODD || F >= kLoraFeatures;
+    const bool active = f0 < F, vectors = ROWS != kShortRows || F >= kLoraFeatures;
     const float scale = TR || u.rank == 0 ? 1.0f : a.scale[u.mat][u.tenant];
 
     int64_t at[4];   // where the lane's results belong: token 4 g + i
@@ -484,7 +495,7 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
     if (y0 && vectors) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) before[i] = load8(y0 + at[i]);
-    } else if (ODD && y0) {
+    } else if (ROWS == kShortRows && y0) {
         const int64_t back = f < F ? 0 : f - (F - 1);   // a lane behind the row reads its last element
 #pragma unroll
         for (int i = 0; i < 4; ++i) before[i] = load8_each(y0 + at[i] - back, F - 1 - f + back);
@@ -492,15 +503,12 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
 #pragma unroll
         for (int i = 0; i < 4; ++i) before[i] = half8{};
     }
-    // Forward: lane and instruction i have piece q = 64 i + lane, 8 ranks of feature q / per_row; the last 8 of a rank that is no multiple of
-    // 8 end with it.  Backward: 8 ranks' rows of A.
+    // Forward: lane and instruction i have piece q = 64 i + lane, 8 ranks of feature q / per_row (and the next feature's first ones, where the
+    // rank is no multiple of 8).  Backward: 8 ranks' rows of A.
     half8 wv[8];
     auto per_row = [&](int r) { return (min(32, u.rank - r) + 7) / 8; };
     auto piece_row = [&](int i, int n) { return (int)(((unsigned)(kWave * i + lane) * (65536u / (unsigned)n + 1)) >> 16); };
-    auto piece_rank = [&](int i, int n, int r) {
-        const int rank = r + 8 * (kWave * i + lane - piece_row(i, n) * n);
-        return ODD ? min(rank, max(u.rank - 8, 0)) : rank;
-    };
+    auto piece_rank = [&](int i, int n, int r) { return r + 8 * (kWave * i + lane - piece_row(i, n) * n); };
     auto load_weights = [&](int r) {
         if constexpr (TR) {
             const int rank = r + 8 * (g & 1), left = u.rank - rank;
@@ -512,8 +520,8 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (i < 2 * n) {
-                    const uint16_t* const w = u.w + min(base + piece_row(i, n), F - 1) * u.rank;
-                    wv[i] = !ODD || u.rank >= 8 ? load8(w + piece_rank(i, n, r)) : load8_each(w, u.rank - 1);
+                    const int64_t at = min(base + piece_row(i, n), F - 1) * u.rank + piece_rank(i, n, r);
+                    wv[i] = ROWS != kEvenRanks ? load8_of<ROWS == kShortRows>(u.w, at, F * u.rank) : load8(u.w + at);
                 }
         }
     };
@@ -587,14 +595,7 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
             for (int i = 0; i < 8; ++i)
                 if (i < 2 * n) {
                     const int row = piece_row(i, n), rank = piece_rank(i, n, r0) - r0;
-                    char* const p = stage + row * 64 + (row >> 3) * 16;
-                    if (!ODD || u.rank % 8 == 0) {
-                        *(half8*)(p + 2 * rank) = wv[i];
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            if (rank + k >= 0 && rank + k < 32) *(_Float16*)(p + 2 * (rank + k)) = wv[i][k];
-                    }
+                    *(half8*)(stage + row * 64 + (row >> 3) * 16 + 2 * rank) = wv[i];
                 }
             __builtin_amdgcn_wave_barrier();
             if (r0 + 32 < padded) load_weights(r0 + 32);
@@ -607,7 +608,7 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
                 for (int j = 0; j < 8; ++j) cols[j] = *(const half8*)(stage + m * (8 * 64 + 16) + j * 64 + half * 32 + (g & 1) * 16);
                 if (u.rank - r < 16) {   // what lies beyond the rank does not count
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) cols[j] = ODD ? only(cols[j], 0, left) : left > 0 ? cols[j] : half8{};
+                    for (int j = 0; j < 8; ++j) cols[j] = ROWS != kEvenRanks ? only(cols[j], 0, left) : left > 0 ? cols[j] : half8{};
                 }
                 product(cols, r);
             }
@@ -640,8 +641,8 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
 // neighbouring lanes would be rows apart and an instruction would take the address unit four times as long.  While a piece is used the
 // next but one is on its way, and the next features' y0.
 constexpr int kPieces = 128 * 32 + 16 * 16;
-template <bool TR, bool ODD>
-__global__ __launch_bounds__(kExpandThreads, ODD ? 2 : 3) void lora_expand_many_kernel(const LoraExpandArgs a) {
+template <bool TR, int ROWS>
+__global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lora_expand_many_kernel(const LoraExpandArgs a) {
     constexpr int kTokens = kLoraExpandTokens, kPer = kExpandThreads / kTokens;   // threads per token while h is prepared
     extern __shared__ __align__(16) char lds[];
     __shared__ float unit[kTokens];
@@ -657,7 +658,7 @@ __global__ __launch_bounds__(kExpandThreads, ODD ? 2 : 3) void lora_expand_many_
     // by element.
     int64_t f0 = (int64_t)blockIdx.y * kLoraFeatures;
     const float scale = TR || u.rank == 0 ? 1.0f : a.scale[u.mat][u.tenant];
-    const bool vectors = !ODD || F >= kLoraFeatures;
+    const bool vectors = ROWS != kShortRows || F >= kLoraFeatures;
     auto begin_of = [&](int64_t first) { return min(first, max(F - kLoraFeatures, (int64_t)0)); };
 
     int64_t row[4];   // the rows of y that the lane's results belong to: token 16 wave + 4 g + i
@@ -678,7 +679,7 @@ __global__ __launch_bounds__(kExpandThreads, ODD ? 2 : 3) void lora_expand_many_
         if (y0 && vectors) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) to[i] = load8(y0 + row[i] + f);
-        } else if (ODD && y0) {
+        } else if (ROWS == kShortRows && y0) {
             const int64_t at = 8 * m < F ? 0 : F - 1 - 8 * m;   // a lane behind the row reads its last element
 #pragma unroll
             for (int i = 0; i < 4; ++i) to[i] = load8_each(y0 + row[i] + at, max(F - 1 - 8 * m, (int64_t)0));
@@ -696,13 +697,10 @@ __global__ __launch_bounds__(kExpandThreads, ODD ? 2 : 3) void lora_expand_many_
             piece = load8(u.w + (int64_t)min(r + piece_row, u.rank - 1) * F + min(f + piece_col, F - 8));
             piece = r + piece_row < u.rank ? piece : half8{};
         } else {
-            const uint16_t* const w = u.w + min(f + piece_row, F - 1) * u.rank;
             const int left = u.rank - r - piece_col;
-            if (!ODD || u.rank % 8 == 0)
-                piece = load8(w + (left > 0 ? r + piece_col : r));
-            else
-                piece = load8_each(w + (left > 0 ? r + piece_col : r), left > 0 ? left - 1 : 0);
-            piece = ODD ? only(piece, 0, left) : left > 0 ? piece : half8{};
+            const int64_t at = min(f + piece_row, F - 1) * u.rank + (left > 0 ? r + piece_col : r);
+            piece = ROWS != kEvenRanks ? load8_of<ROWS == kShortRows>(u.w, at, F * u.rank) : load8(u.w + at);
+            piece = ROWS != kEvenRanks ? only(piece, 0, left) : left > 0 ? piece : half8{};
         }
     };
     // the pieces come in the order of their use: 16 ranks after 16 ranks, then the next features; past the end the last once more
@@ -1073,7 +1071,7 @@ hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transpo
 
 hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int max_rank, int64_t min_F, int64_t max_F, bool odd, hipStream_t st) {
     if (a.n_tiles < 1 || max_rank > kLoraMaxRank || a.splits > kLoraMaxSplits) return hipErrorInvalidValue;
-    odd = (odd && !transposed) || min_F < kLoraFeatures;
+    const int rows = min_F < kLoraFeatures ? kShortRows : odd && !transposed ? kOddRanks : kEvenRanks;
     const int64_t wide = std::max<int64_t>(1, (max_F + kLoraFeatures - 1) / kLoraFeatures);   // (F = 0: h alone)
     if (columns == 16) {
         const int64_t groups = (wide + kLoraExpandWaves - 1) / kLoraExpandWaves;
@@ -1083,21 +1081,23 @@ hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transpo
             hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)groups), dim3(kExpandThreads), lds, st, a);
             return hipGetLastError();
         };
-        return transposed ? (odd ? go(lora_expand_few_kernel<true, true>) : go(lora_expand_few_kernel<true, false>)) : odd ? go(lora_expand_few_kernel<false, true>) : go(lora_expand_few_kernel<false, false>);
+        if (transposed) return rows == kShortRows ? go(lora_expand_few_kernel<true, kShortRows>) : go(lora_expand_few_kernel<true, kEvenRanks>);
+        return rows == kShortRows ? go(lora_expand_few_kernel<false, kShortRows>) : rows == kOddRanks ? go(lora_expand_few_kernel<false, kOddRanks>) : go(lora_expand_few_kernel<false, kEvenRanks>);
     }
     int cus = 256;
     if (const hipError_t e = device_cu_count(&cus); e != hipSuccess) return e;
     // as many workgroups as run at a time (forward 4 to a compute unit, backward 3), each taking several turns
     const int64_t turns = std::max<int64_t>(1, std::min<int64_t>(wide, (int64_t)(transposed ? 3 : 4) * cus / a.n_tiles));
     const unsigned lds = (unsigned)(2 * kPieces + 2 * kLoraExpandTokens * (((max_rank + 15) & ~15) + 8) * 2);
-    static PerDeviceOnce once[4];
+    static PerDeviceOnce once[5];
     auto go = [&](auto kernel, int which) {
         const hipError_t e = once[which].run([&] { return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kPieces + 2 * kLoraExpandTokens * (kLoraMaxRank + 8) * 2); });
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)turns), dim3(kExpandThreads), lds, st, a);
         return hipGetLastError();
     };
-    return transposed ? (odd ? go(lora_expand_many_kernel<true, true>, 0) : go(lora_expand_many_kernel<true, false>, 1)) : odd ? go(lora_expand_many_kernel<false, true>, 2) : go(lora_expand_many_kernel<false, false>, 3);
+    if (transposed) return rows == kShortRows ? go(lora_expand_many_kernel<true, kShortRows>, 0) : go(lora_expand_many_kernel<true, kEvenRanks>, 1);
+    return rows == kShortRows ? go(lora_expand_many_kernel<false, kShortRows>, 2) : rows == kOddRanks ? go(lora_expand_many_kernel<false, kOddRanks>, 3) : go(lora_expand_many_kernel<false, kEvenRanks>, 4);
 }
 
 hipError_t launch_lora_prep(const LoraPrepArgs& a, int chunks, int sides, hipStream_t st) {
