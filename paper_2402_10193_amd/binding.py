@@ -880,7 +880,7 @@ LORA_MAX_RANK = 256
 
 def _here(*tensors) -> None:
     """The tensors of a call are on the current device: its kernels run there."""
-    dev = torch.cuda.current_device() if _current_device is None or not torch.cuda.is_initialized() else _current_device()
+    dev = torch.cuda.current_device() if _current_device is None else _current_device()   # (there is a device: tensors are on one)
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
@@ -890,7 +890,7 @@ def _tok_pointer(tenant_of_token, T: int):
     """The tokens' tenants as the library takes them, and what keeps them alive: a CPU int32 tensor is passed as it is."""
     if isinstance(tenant_of_token, torch.Tensor):
         t = tenant_of_token
-        if t.device.type != "cpu" or t.dtype != torch.int32 or not t.is_contiguous():
+        if t.is_cuda or t.dtype is not torch.int32 or not t.is_contiguous():
             raise TypeError("tenant_of_token: a sequence of ints or a contiguous int32 CPU tensor")
         n, keep, p = t.numel(), t, t.data_ptr()
     else:
@@ -968,18 +968,34 @@ class LoraGroup:
         self.a_ptrs = (ctypes.c_void_p * size)(*flat(lambda t: t.a_ptrs))
         self.b_ptrs = (ctypes.c_void_p * size)(*flat(lambda t: t.b_ptrs))
         self.rank_arr = (ctypes.c_int32 * size)(*flat(lambda t: t.rank_arr))
-        self.scale = (ctypes.c_void_p * self.n)(*[_ptr(t.scale) or None for t in self.tables])
+        self.scales, self.array = [t.scale for t in self.tables], ctypes.c_void_p * self.n
+        self.scale = self.array(*[_ptr(t) or None for t in self.scales])
         self.out_arr = (ctypes.c_int64 * self.n)(*self.outs)
 
 
-def _lora_rows(t: Optional[torch.Tensor], T: int, width: int, what: str) -> None:
-    if t is not None:
-        _dev(t, torch.float16, what)
-        if tuple(t.shape) != (T, width):
-            raise ValueError(f"{what} must be [{T}, {width}]")
+def _arg(t: Optional[torch.Tensor], dtype, shape, dev: int, what: str) -> int:
+    """The address of a call's tensor after its checks, 0 for None: made in one go, and looked at one by one only where something is wrong."""
+    if t is None:
+        return 0
+    if t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    _dev(t, dtype, what)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {list(shape)}")
+    raise ValueError(f"{what} is on {t.device}, the current device is cuda:{dev}")
+
+
+def _device_of(t: torch.Tensor, what: str) -> int:
+    """The device of a call: its first tensor's, which is the current one."""
+    dev = _dev(t, torch.float16, what).get_device()
+    _here(t)
+    if t.dim() != 2:
+        raise ValueError(f"{what} is a matrix")
+    return dev
 
 
 def _lora_h(h: Optional[torch.Tensor], T: int) -> int:
+    """Its width."""
     if h is None:
         return 0
     _dev(h, torch.float32, "h")
@@ -994,23 +1010,26 @@ def lora_multitenant(x: torch.Tensor, adapters: LoraTable, tenant_of_token, y0: 
     """bd_lora_multitenant: y fp16 [T, out] = y0 + what every token's adapter adds.  y0: what the shared projection gave (None: zeros;
     y=y0: in place).  h: float32 [T, >= largest rank] that receives A x for the backward pass.  tenant_of_token: a sequence, or a CPU
     int32 tensor (no conversion).  out: needed only where no tenant has an adapter and neither y0 nor y is given."""
-    _dev(x, torch.float16, "x")
+    dev = _device_of(x, "x")
     T, inn = x.shape
-    out = next((int(t.shape[1]) for t in (y, y0) if t is not None), adapters.shape[0] if adapters.shape else out)
-    if out is None or (adapters.shape is not None and adapters.shape != (out, inn)):
+    for t in (y0, y):
+        if t is not None and t.dim() == 2:
+            out = t.shape[1]
+    if adapters.shape is not None:
+        out = adapters.shape[0]
+    if out is None or (adapters.shape is not None and adapters.shape[1] != inn):
         raise ValueError("x, y and the adapters disagree in shape")
     if y is None:
         y = torch.empty((T, out), dtype=torch.float16, device=x.device)
-    _lora_rows(y, T, out, "y")
-    _lora_rows(y0, T, out, "y0")
-    h_ld = _lora_h(h, T)
     if workspace is None:
         workspace = new_workspace(lora_workspace_bytes(T, 1, adapters.max_rank), x.device)
-    _here(x, y, y0, h, workspace, adapters.scale)
+    h_ld = _lora_h(h, T)
+    _here(h, workspace, adapters.scale)
     tok, keep = _tok_pointer(tenant_of_token, T)
-    _check(lib().bd_lora_multitenant(_ptr(x), adapters.a_ptrs, adapters.b_ptrs, adapters.rank_arr, _ptr(adapters.scale), tok, _ptr(y0),
-                                     _ptr(y), _ptr(h), h_ld, T, out, inn, adapters.n_tenants, _ptr(workspace), workspace.numel(),
-                                     _stream(stream)), "bd_lora_multitenant")
+    _check(lib().bd_lora_multitenant(x.data_ptr(), adapters.a_ptrs, adapters.b_ptrs, adapters.rank_arr, adapters.scale.data_ptr(), tok,
+                                     _arg(y0, torch.float16, (T, out), dev, "y0"), _arg(y, torch.float16, (T, out), dev, "y"), _ptr(h), h_ld,
+                                     T, out, inn, adapters.n_tenants, workspace.data_ptr(), workspace.numel(), _stream(stream)),
+           "bd_lora_multitenant")
     return y
 
 
@@ -1018,7 +1037,7 @@ def lora_multitenant_group(x: torch.Tensor, group: LoraGroup, tenant_of_token, y
                            ys: Optional[Sequence[torch.Tensor]] = None, hs: Optional[Sequence[torch.Tensor]] = None,
                            workspace: Optional[torch.Tensor] = None, stream=None):
     """bd_lora_multitenant_group: list of y_m fp16 [T, out_m].  hs: all or none, of one width."""
-    _dev(x, torch.float16, "x")
+    dev = _device_of(x, "x")
     T, inn = x.shape
     if group.inn is not None and group.inn != inn:
         raise ValueError("x and the adapters disagree on `in`")
@@ -1027,20 +1046,23 @@ def lora_multitenant_group(x: torch.Tensor, group: LoraGroup, tenant_of_token, y
     y0s = list(y0s) if y0s is not None else [None] * group.n
     if len(ys) != group.n or len(y0s) != group.n or (hs is not None and len(hs) != group.n):
         raise ValueError("one y (y0, h) per matrix")
-    for y, y0, o in zip(ys, y0s, group.outs):
-        _lora_rows(y, T, o, "y")
-        _lora_rows(y0, T, o, "y0")
-    widths = {_lora_h(h, T) for h in hs} if hs is not None else {0}
-    if len(widths) > 1:
-        raise ValueError("h of one width")
+    f16, array = torch.float16, group.array
+    y_ptrs = array(*[_arg(y, f16, (T, o), dev, "y") or None for y, o in zip(ys, group.outs)])
+    y0_ptrs = array(*[_arg(y0, f16, (T, o), dev, "y0") or None for y0, o in zip(y0s, group.outs)])
+    h_ptrs, h_ld = None, 0
+    if hs is not None:
+        widths = {_lora_h(h, T) for h in hs}
+        if len(widths) > 1:
+            raise ValueError("h of one width")
+        _here(*hs)
+        h_ptrs, h_ld = array(*[_ptr(h) or None for h in hs]), widths.pop()
     if workspace is None:
         workspace = new_workspace(lora_workspace_bytes(T, group.n, group.max_rank), x.device)
-    _here(x, *ys, *y0s, *(hs or ()), workspace, *[t.scale for t in group.tables])
+    _here(workspace, *group.scales)
     tok, keep = _tok_pointer(tenant_of_token, T)
-    ptrs = lambda ts: (ctypes.c_void_p * group.n)(*[_ptr(t) or None for t in ts])
-    _check(lib().bd_lora_multitenant_group(group.n, _ptr(x), group.a_ptrs, group.b_ptrs, group.rank_arr, group.scale, tok, ptrs(y0s),
-                                           ptrs(ys), ptrs(hs) if hs is not None else None, widths.pop(), T, group.out_arr, inn,
-                                           group.n_tenants, _ptr(workspace), workspace.numel(), _stream(stream)),
+    _check(lib().bd_lora_multitenant_group(group.n, x.data_ptr(), group.a_ptrs, group.b_ptrs, group.rank_arr, group.scale, tok, y0_ptrs,
+                                           y_ptrs, h_ptrs, h_ld, T, group.out_arr, inn, group.n_tenants, workspace.data_ptr(),
+                                           workspace.numel(), _stream(stream)),
            "bd_lora_multitenant_group")
     return list(ys)
 
@@ -1069,7 +1091,7 @@ def lora_multitenant_backward(dy: torch.Tensor, x: Optional[torch.Tensor], h: Op
                               want_dx: bool = True, accumulate: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
     """bd_lora_multitenant_backward: fills `grads` (accumulate: adds to them) and returns dx fp16 [T, in] = dx0 + what comes through the
     adapters (None if want_dx is False).  x, h: what the forward call had and gave; x may be None where no dA, h where no dB is wanted."""
-    _dev(dy, torch.float16, "dy")
+    dev = _device_of(dy, "dy")
     T, out = dy.shape
     if adapters.shape is None:
         raise ValueError("no tenant has an adapter")
@@ -1080,17 +1102,17 @@ def lora_multitenant_backward(dy: torch.Tensor, x: Optional[torch.Tensor], h: Op
         dx = torch.empty((T, inn), dtype=torch.float16, device=dy.device)
     if not want_dx:
         dx = dx0 = None
-    for t, what in ((x, "x"), (dx0, "dx0"), (dx, "dx")):
-        _lora_rows(t, T, inn, what)
+    f16, shape = torch.float16, (T, inn)
+    x_ptr, dx0_ptr, dx_ptr = _arg(x, f16, shape, dev, "x"), _arg(dx0, f16, shape, dev, "dx0"), _arg(dx, f16, shape, dev, "dx")
     h_ld = _lora_h(h, T)
     if workspace is None:
         workspace = new_workspace(lora_backward_workspace_bytes(T, out, inn, adapters.n_tenants, adapters.max_rank), dy.device)
-    _here(dy, x, h, dx0, dx, workspace, adapters.scale)
+    _here(h, workspace, adapters.scale)
     tok, keep = _tok_pointer(tenant_of_token, T)
-    _check(lib().bd_lora_multitenant_backward(_ptr(dy), _ptr(x), _ptr(h), h_ld, adapters.a_ptrs, adapters.b_ptrs, adapters.rank_arr,
-                                              _ptr(adapters.scale), tok, _ptr(dx0), _ptr(dx), grads.da_ptrs if grads else None,
+    _check(lib().bd_lora_multitenant_backward(dy.data_ptr(), x_ptr, _ptr(h), h_ld, adapters.a_ptrs, adapters.b_ptrs, adapters.rank_arr,
+                                              adapters.scale.data_ptr(), tok, dx0_ptr, dx_ptr, grads.da_ptrs if grads else None,
                                               grads.db_ptrs if grads else None, int(accumulate), T, out, inn, adapters.n_tenants,
-                                              _ptr(workspace), workspace.numel(), _stream(stream)), "bd_lora_multitenant_backward")
+                                              workspace.data_ptr(), workspace.numel(), _stream(stream)), "bd_lora_multitenant_backward")
     return dx
 
 
