@@ -676,9 +676,9 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     const uint16_t* const y0 = a.y0[u.mat];
     half8 before[4];
     auto load_y0 = [&](half8 (&to)[4], int64_t f) {
-        if (y0 && vectors) {
+        if (vectors) {   // (without y0 something that is in the cache: no branch)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) to[i] = load8(y0 + row[i] + f);
+            for (int i = 0; i < 4; ++i) to[i] = load8(y0 ? y0 + row[i] + f : a.y[u.mat] + 8 * m);
         } else if (ROWS == kShortRows && y0) {
             const int64_t at = 8 * m < F ? 0 : F - 1 - 8 * m;   // a lane behind the row reads its last element
 #pragma unroll
@@ -692,16 +692,19 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     const int piece_row = TR ? (int)threadIdx.x >> 4 : (int)threadIdx.x >> 1, piece_col = TR ? 8 * ((int)threadIdx.x & 15) : 8 * ((int)threadIdx.x & 1);
     char* const piece_at = pieces + (TR ? piece_row * 272 + piece_col * 2 : piece_row * 32 + piece_col * 2 + (piece_row >> 3) * 16);
     half8 piece;
+    int piece_left = 0;   // ranks of it that count (backward: whether it does); looked at when it goes to LDS, so that nothing waits for the load
     auto load_piece = [&](int64_t f, int r) {
         if constexpr (TR) {   // (F = in, a multiple of 32)
+            piece_left = u.rank - r - piece_row;
             piece = load8(u.w + (int64_t)min(r + piece_row, u.rank - 1) * F + min(f + piece_col, F - 8));
-            piece = r + piece_row < u.rank ? piece : half8{};
         } else {
-            const int left = u.rank - r - piece_col;
-            const int64_t at = min(f + piece_row, F - 1) * u.rank + (left > 0 ? r + piece_col : r);
+            piece_left = u.rank - r - piece_col;
+            const int64_t at = min(f + piece_row, F - 1) * u.rank + (piece_left > 0 ? r + piece_col : r);
             piece = ROWS != kEvenRanks ? load8_of<ROWS == kShortRows>(u.w, at, F * u.rank) : load8(u.w + at);
-            piece = ROWS != kEvenRanks ? only(piece, 0, left) : left > 0 ? piece : half8{};
         }
+    };
+    auto put_piece = [&](int buffer, half8 v, int left) {
+        *(half8*)(piece_at + buffer * kPieces) = !TR && ROWS != kEvenRanks ? only(v, 0, left) : left > 0 ? v : half8{};
     };
     // the pieces come in the order of their use: 16 ranks after 16 ranks, then the next features; past the end the last once more
     int64_t piece_f0 = f0;
@@ -716,9 +719,16 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
         }
     };
     const bool work = f0 < F;   // (not for a matrix without outputs, whose h alone is asked for)
+    half8 piece0 = {};
+    int left0 = 0;
     if (work) {
+        if (padded > 0) {   // two pieces before h: nothing is in flight when the turns begin
+            next_piece();
+            piece0 = piece;
+            left0 = piece_left;
+            next_piece();
+        }
         load_y0(before, begin_of(f0));
-        if (padded > 0) next_piece();
     }
 
     // h of the tile's tokens: the parts added up, the exponent, hi and lo into LDS
@@ -761,10 +771,7 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
         *(half4*)(lo + c * pitch + r) = l;
     }
     if (!work) return;   // (of the whole workgroup)
-    if (padded > 0) {
-        *(half8*)piece_at = piece;
-        next_piece();
-    }
+    if (padded > 0) put_piece(0, piece0, left0);
     __syncthreads();
 
     uint16_t* const y = a.y[u.mat];
@@ -776,8 +783,8 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     for (; f0 < F; f0 += stride) {
         const int64_t f = begin_of(f0), fl = f + 8 * m;
         float4v acc[8] = {};
-        for (int r = 0; r < padded; r += 16) {
-            *(half8*)(piece_at + (buffer ^ 1) * kPieces) = piece;   // of the next ranks or features
+        auto step = [&](int r) {
+            put_piece(buffer ^ 1, piece, piece_left);   // of the next ranks or features
             next_piece();
             const char* const at = pieces + buffer * kPieces + (TR ? 8 * (g & 1) * 272 + m * 16 : m * (8 * 32 + 16) + (g & 1) * 16);
             half8 wv[8], cols[8];
@@ -794,23 +801,27 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
             for (int j = 0; j < 8; ++j) acc[j] = mfma(hv, cols[j], acc[j]);
             buffer ^= 1;
             __syncthreads();
-        }
+        };
+        if (padded > 0) step(0);   // (not in the loop: what is in flight is known at each of its waits)
+        for (int r = 16; r < padded; r += 16) step(r);
+        half8 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = (_Float16)__builtin_fmaf(acc[j][i], up[i], y0 ? (float)before[i][j] : 0.0f);
+        // the next y0 is asked for before the stores: no wait for it has to wait for them (past the end: the last features' once more)
+        load_y0(before, begin_of(min(f0 + stride, F - 1)));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            half8 v;
+            if (16 * wave + 4 * g + i >= u.count) continue;
+            if (fl >= f0 && F - fl >= 8) {
+                __builtin_memcpy(y + row[i] + f, &v[i], 16);
+            } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (_Float16)__builtin_fmaf(acc[j][i], up[i], (float)before[i][j]);
-            if (16 * wave + 4 * g + i < u.count) {
-                if (fl >= f0 && F - fl >= 8) {
-                    __builtin_memcpy(y + row[i] + f, &v, 16);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (fl + j >= f0 && fl + j < F) *(_Float16*)(y + row[i] + f + j) = v[j];
-                }
+                for (int j = 0; j < 8; ++j)
+                    if (fl + j >= f0 && fl + j < F) *(_Float16*)(y + row[i] + f + j) = v[i][j];
             }
         }
-        load_y0(before, begin_of(min(f0 + stride, F - 1)));   // (past the end: the last features' once more)
     }
 }
 
@@ -1086,8 +1097,9 @@ hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transpo
     }
     int cus = 256;
     if (const hipError_t e = device_cu_count(&cus); e != hipSuccess) return e;
-    // as many workgroups as run at a time (forward 4 to a compute unit, backward 3), each taking several turns
-    const int64_t turns = std::max<int64_t>(1, std::min<int64_t>(wide, (int64_t)(transposed ? 3 : 4) * cus / a.n_tiles));
+    // as many workgroups as run at a time (forward 4 to a compute unit, backward 3), each taking the same number of turns
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(wide, (int64_t)(transposed ? 3 : 4) * cus / a.n_tiles));
+    const int64_t each = (wide + most - 1) / most, turns = (wide + each - 1) / each;
     const unsigned lds = (unsigned)(2 * kPieces + 2 * kLoraExpandTokens * (((max_rank + 15) & ~15) + 8) * 2);
     static PerDeviceOnce once[5];
     auto go = [&](auto kernel, int which) {
