@@ -103,9 +103,8 @@ __device__ __forceinline__ Where find_tile(const Args& a, int t) {
         const LoraTile& k = a.tile[t];
         u = Where{k.w, k.hrow, k.tenant, k.count, k.rank, k.mat, 0, t};
     } else {
-        int j = 0;
-#pragma unroll
-        for (int k = 1; k < kLoraRecords; ++k) j += t >= a.jobs.tile_begin[k] ? 1 : 0;
+        // a lane looks at a record: few instructions (a kernel's code, too, comes out of memory when it begins)
+        const int j = __builtin_amdgcn_readfirstlane(__popcll(__ballot(t >= a.jobs.tile_begin[threadIdx.x & (kWave - 1)])) - 1);
         const LoraJob& k = a.jobs.job[j];
         const int skip = (t - a.jobs.tile_begin[j]) * 16 * NT;
         u = Where{k.w, k.hrow + skip, k.tenant, min(k.count - skip, 16 * NT), k.rank, k.mat, k.first + skip, j};
@@ -324,8 +323,9 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
         if constexpr (TR) {
             const int at = lane + kWave * r, per_row = width / 8;
             // (a lane without a piece of its own reads and stores one of the last row's once more: no branches)
-            piece_row[r] = pieces ? min(at / per_row, 31) : 0;
-            piece_col[r] = pieces ? 8 * (at % per_row) : 0;
+            const int over = (int)(((unsigned)at * (65536u / (unsigned)per_row + 1)) >> 16);   // at / per_row
+            piece_row[r] = pieces ? min(over, 31) : 0;
+            piece_col[r] = pieces ? 8 * (at - over * per_row) : 0;
             wrow[r] = u.w + 16 * rt0 + piece_col[r];
         } else {
             const int rank = 16 * (rt0 + r) + mr < u.rank ? 16 * (rt0 + r) + mr : 0;
@@ -831,8 +831,8 @@ constexpr int kPrepThreads = 256;
 // exponent for the 32.  Lane (n, q) holds rank n of its 16, tokens 8 q .. 8 q + 7, in 16 bytes.  Where g came in parts their sum
 // takes the first part's place.
 __global__ __launch_bounds__(kPrepThreads) void lora_prep_kernel(const LoraPrepArgs a) {
-    int j = 0;
-    while (j + 1 < a.n_jobs && a.job[j + 1].chunk_begin <= (int)blockIdx.x + a.chunk_first) ++j;
+    const int record = threadIdx.x & (kWave - 1);
+    const int j = __builtin_amdgcn_readfirstlane(__popcll(__ballot(record < a.n_jobs && a.job[min(record, a.n_jobs - 1)].chunk_begin <= (int)blockIdx.x + a.chunk_first)) - 1);
     const LoraPrepJob& job = a.job[j];
     const bool of_h = blockIdx.y + a.side_first == 1;
     const int chunk = blockIdx.x + a.chunk_first, t0 = (chunk - job.chunk_begin) * 32, rank_all = job.rank, tiles = (rank_all + 15) / 16;
@@ -922,9 +922,8 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(OD
     __shared__ uint16_t ids[kLoraPartTokens];
     const int which = (int)blockIdx.z >= a.rank_groups ? 1 : 0, rt0 = ((int)blockIdx.z - which * a.rank_groups) * RW;
     const LoraGradSide& side = a.side[which];
-    int which_job = 0;
-#pragma unroll
-    for (int k = 1; k < kLoraGradJobs; ++k) which_job += (int)blockIdx.y >= a.part_begin[k] ? 1 : 0;
+    const int record = threadIdx.x & (kWave - 1);
+    const int which_job = __builtin_amdgcn_readfirstlane(__popcll(__ballot(record < kLoraGradJobs && (int)blockIdx.y >= a.part_begin[min(record, kLoraGradJobs - 1)])) - 1);
     const LoraGradJob& job = a.job[which_job];
     const int split = blockIdx.y - a.part_begin[which_job], rank_all = job.rank;
     float* const result = job.out[which];
