@@ -28,7 +28,7 @@ namespace bd {
 
 namespace {
 
-constexpr float kAvgTop = 1984.0f, kSqTop = 4032.0f;   // 31 * 2^6, 63 * 2^6
+constexpr float kAvgTop = 1984.0f, kSqTop = 4032.0f;   // 31 * 2^6, 63 * 2^6; scales are products with their reciprocals
 
 // value of a code without its sign; F fraction bits
 template <int F>
@@ -199,8 +199,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwArgs a) {
             rt = wave_max(rt);
             // a block with an infinity or a NaN is NaN; one whose largest |m| is below 2^-100 is zero
             const bool m_ok = mt < 0x7f800000u, r_ok = rt < 0x7f800000u, m_any = m_ok && mt >= (27u << 23), r_any = r_ok && rt > 0;
-            const float m_scale = !m_ok ? __builtin_nanf("") : m_any ? __uint_as_float(mt) / kAvgTop : 0.0f;
-            const float v_scale = !r_ok ? __builtin_nanf("") : r_any ? __uint_as_float(rt) / kSqTop : 0.0f;
+            const float m_scale = !m_ok ? __builtin_nanf("") : m_any ? __uint_as_float(mt) * (1.0f / kAvgTop) : 0.0f;
+            const float v_scale = !r_ok ? __builtin_nanf("") : r_any ? __uint_as_float(rt) * (1.0f / kSqTop) : 0.0f;
             const float my = m_any ? 1.0f / m_scale : 0.0f, vy = r_any ? 1.0f / v_scale : 0.0f;
             uint32_t mo = 0, vo = 0;
 #pragma unroll
@@ -287,7 +287,7 @@ bd_status make_plan(void* plan, size_t plan_bytes, int32_t n, float* const* para
     using bd::misaligned;
     if (n < 0 || n > BD_ADAMW_MAX_TENSORS) return BD_ERR_SHAPE;
     if (!plan) return BD_ERR_NULL;
-        if (misaligned(plan, 8)) return BD_ERR_ALIGN;
+    if (misaligned(plan, 8)) return BD_ERR_ALIGN;
     if (n > 0 && !numel) return BD_ERR_NULL;
     for (int32_t i = 0; i < n; ++i)
         if (numel[i] < 0 || numel[i] > BD_ADAMW_MAX_ELEMENTS) return BD_ERR_SHAPE;
