@@ -984,13 +984,14 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(OD
         if (now >= largest - 64) {
             largest = max(largest, now);
             if (now != e && e > -200) {
-                const float f = e - now < -126 ? 0.0f : power_of_two(e - now);
+                const float f = power_of_two(max(e - now, -126));   // (not zero: an infinity stays one)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[j] *= f;
             }
             e = now;
-        } else {   // too small to count
-            op[b][0] = half8{};
+        } else {   // too small to count, but for infinities and NaN
+#pragma unroll
+            for (int i = 0; i < 8; ++i) op[b][0][i] = finite((float)op[b][0][i]) ? (_Float16)0.0f : op[b][0][i];
             op[b][1] = half8{};
         }
 #pragma unroll

@@ -1,0 +1,94 @@
+"""Edges of the low-rank adapters' calls: gradients with infinities in tokens whose other values are far below the rest, signs of zero
+of tokens without an adapter, many tenants of one token, the routes of two tokens per tenant."""
+import pytest
+import torch
+
+import lora_ref as ref64
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def bd():
+    from paper_2402_10193_amd import binding
+    return binding
+
+
+def _adapters(ranks, out, inn, gen):
+    a = [(torch.randn(r, inn, generator=gen) * inn ** -0.5).half().to(DEV) if r else None for r in ranks]
+    b = [(torch.randn(out, r, generator=gen) * 0.2).half().to(DEV) if r else None for r in ranks]
+    return a, b
+
+
+@pytest.mark.parametrize("T,rank,chunk", [(96, 8, 1), (700, 8, 1), (4000, 64, 19), (20000, 8, 19)])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_gradients_keep_what_is_not_finite(bd, T, rank, chunk, bad):
+    """32 tokens whose dy (and h) are zero but for one value that is not finite, beside tokens of ordinary size: that value's rows of dA
+    and columns of dB are not finite, all others are those without it."""
+    gen = torch.Generator().manual_seed(5)
+    out, inn, first = 256, 128, 32 * chunk
+    a, b = _adapters([rank], out, inn, gen)
+    table = bd.LoraTable(a, b, [1.0])
+    x = torch.randn(T, inn, generator=gen).half().to(DEV)
+    dy = torch.randn(T, out, generator=gen).half().to(DEV) * 64
+    h = torch.randn(T, rank, generator=gen).to(DEV) * 4096
+    dy[first:first + 32] = 0
+    h[first:first + 32] = 0
+    grads = lambda: ([torch.zeros(rank, inn, device=DEV)], [torch.zeros(out, rank, device=DEV)])
+    (da,), (db,) = want = grads()
+    bd.lora_multitenant_backward(dy, x, h, table, [0] * T, bd.LoraGrads(table, *want), want_dx=False)
+    dy2, h2 = dy.clone(), h.clone()
+    dy2[first + 8, 3] = bad                                 # g of this token is not finite
+    h2[first + 18, 2] = bad                                  # dB's column 2
+    (da2,), (db2,) = got = grads()
+    bd.lora_multitenant_backward(dy2, x, h2, table, [0] * T, bd.LoraGrads(table, *got), want_dx=False)
+    assert torch.isfinite(da).all() and torch.isfinite(db).all()
+    assert not torch.isfinite(da2).any()
+    assert not torch.isfinite(db2[:, 2]).any() and not torch.isfinite(db2[3]).any()
+    rows = [r for r in range(out) if r != 3]
+    for column in (0, 1, 3, 7):
+        assert torch.equal(db2[rows, column], db[rows, column])
+
+
+@pytest.mark.parametrize("T", [2, 40, 600])
+def test_tokens_without_an_adapter_keep_their_bits(bd, T):
+    gen = torch.Generator().manual_seed(6)
+    a, b = _adapters([8, 0], 136, 64, gen)
+    table = bd.LoraTable(a, b, [1.0, float("nan")])
+    x = torch.randn(T, 64, generator=gen).half().to(DEV)
+    y0 = torch.randn(T, 136, generator=gen).half().to(DEV)
+    y0[:, ::7], y0[:, 1::7] = -0.0, 0.0
+    y0[1, 5], y0[1, 6] = float("inf"), -float("inf")
+    tok = [t % 2 for t in range(T)]
+    y = bd.lora_multitenant(x, table, tok, y0=y0)
+    assert torch.equal(y[1::2].view(torch.int16), y0[1::2].view(torch.int16))
+    dx0 = torch.randn(T, 64, generator=gen).half().to(DEV)
+    dx0[:, ::5] = -0.0
+    dx = bd.lora_multitenant_backward(y0, None, None, table, tok, None, dx0=dx0)
+    assert torch.equal(dx[1::2].view(torch.int16), dx0[1::2].view(torch.int16))
+
+
+@pytest.mark.parametrize("per_tenant", [1, 2, 3])
+@pytest.mark.parametrize("ranks", [[16, 8], [16, 0, 5, 1], [17, 16]])
+def test_many_tenants_of_few_tokens(bd, ranks, per_tenant):
+    """More (tenant, matrix) pairs than one launch takes; ranks and tokens on both sides of what one launch of both products takes."""
+    gen = torch.Generator().manual_seed(7)
+    n, out, inn = 150, 200, 96
+    ranks = [ranks[e % len(ranks)] for e in range(n)]
+    T = n * per_tenant
+    tok = [(7 * t) % n for t in range(T)]
+    a, b = _adapters(ranks, out, inn, gen)
+    scale = torch.rand(n, generator=gen) + 0.5
+    table = bd.LoraTable(a, b, scale)
+    x = torch.randn(T, inn, generator=gen).half().to(DEV)
+    y0 = torch.randn(T, out, generator=gen).half().to(DEV)
+    h = torch.full((T, max(ranks)), 7.0, device=DEV)
+    y = bd.lora_multitenant(x, table, tok, y0=y0, h=h)
+    want, h_of, bound = ref64.forward(x, a, b, scale, tok, y0, out)
+    ref64.check(y, want, bound, "y")
+    for e, (rows, want_h) in h_of.items():
+        size = x[rows].double().abs() @ a[e].double().abs().t()
+        ref64.check(h[rows, :ranks[e]], want_h, (inn / 8 + 16) * ref64.U32 * size, f"h of tenant {e}")
+    for t, e in enumerate(tok):
+        assert (h[t, ranks[e]:] == 7.0).all()
