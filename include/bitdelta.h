@@ -439,17 +439,18 @@ bd_status bd_linear_multitenant_tiled_group_q8(int32_t n_mats, const uint16_t* x
  *   x_f16            [T, in]
  *   a_by_tenant, b_by_tenant   HOST arrays of n_tenants DEVICE pointers; NULL allowed for tenants without a token and where
  *                    the rank is 0
- *   rank_by_tenant   HOST [n_tenants], 0 .. BD_LORA_MAX_RANK each (checked for tenants with a token); 0: no adapter, y[t] = y0[t]
+ *   rank_by_tenant   HOST [n_tenants], 0 .. BD_LORA_MAX_RANK each (checked for tenants with a token); 0: no adapter, y[t] = y0[t] bit by bit
  *   scale_by_tenant  device array of n_tenants floats
  *   tenant_of_token  HOST [T], any order; tokens are grouped by tenant inside the call
  *   y0_f16, y_f16    [T, out]; y0 may be NULL (zeros) or y itself, but not overlap y otherwise
  *   h                NULL, or device [T, h_ld] floats that receive h[t][0 .. r_e) for the backward pass; h_ld >= the largest rank
  *                    of the call's tokens; entries beyond a token's rank are left as they were
- *   workspace        bd_lora_workspace_bytes(T, 1, largest rank) bytes, 256-byte aligned, device memory: holds h between the two
- *                    launches (one call at a time per workspace; not needed where no token has an adapter)
- * in % 32 == 0, out and in up to 2^24; T up to 65535, more than 64 tenants (16-token runs of tenants up to T = 512) run as several
- * pairs of launches.  The sum over `in` is cut by a rule on the sizes of the call, so the last bits of h may change with the other
- * tokens of the call.  No tensor that is written may overlap any other (BD_ERR_ALIAS). */
+ *   workspace        bd_lora_workspace_bytes(T, 1, largest rank) bytes, 256-byte aligned, device memory: holds the order of the
+ *                    tokens and h between the launches (one call at a time per workspace; not needed where no token has an adapter)
+ * in % 32 == 0, out and in up to 2^24, T up to 65535.  One or two tokens per tenant with ranks up to 16 (a decode step) run as one
+ * launch for 112 tenants, else a launch for each product and 64 tenants (up to T = 512: runs of 16 tokens of a tenant).  The sum over
+ * `in` is cut by a rule on the sizes of the call, so the last bits of h may change with the other tokens of the call.  No tensor that
+ * is written may overlap any other (BD_ERR_ALIAS). */
 #define BD_LORA_MAX_RANK 256
 size_t bd_lora_workspace_bytes(int64_t T, int32_t n_mats, int32_t max_rank);
 bd_status bd_lora_multitenant(const uint16_t* x_f16, const uint16_t* const* a_by_tenant, const uint16_t* const* b_by_tenant,

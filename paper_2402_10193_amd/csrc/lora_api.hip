@@ -188,6 +188,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
         if (overlaps(y[m], ybytes, x, xbytes) || (hbytes && (overlaps(h[m], hbytes, x, xbytes) || overlaps(h[m], hbytes, y[m], ybytes)))) return BD_ERR_ALIAS;
         for (int o = 0; o < n_mats; ++o) {
             const size_t obytes = (size_t)T * out[o] * 2;
+            if (max_rank > 0 && scale[o] && (overlaps(y[m], ybytes, scale[o], (size_t)n_tenants * 4) || (hbytes && overlaps(h[m], hbytes, scale[o], (size_t)n_tenants * 4)))) return BD_ERR_ALIAS;
             if (o != m && overlaps(y[m], ybytes, y[o], obytes)) return BD_ERR_ALIAS;
             if (o != m && hbytes && (overlaps(h[m], hbytes, y[o], obytes) || (h[o] && overlaps(h[m], hbytes, h[o], (size_t)T * h_ld * 4)))) return BD_ERR_ALIAS;
             if (y0 && y0[o] && !(o == m && y0[m] == y[m]) && overlaps(y[m], ybytes, y0[o], obytes)) return BD_ERR_ALIAS;
@@ -390,6 +391,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
     range(dy, (size_t)T * out * 2, false);
     range(x, (size_t)T * in * 2, false);
     if (any_db) range(h, (size_t)T * h_ld * 4, false);
+    if (work) range(scale, (size_t)n_tenants * 4, false);
     if (want_dx) {
         range(dx, (size_t)T * in * 2, true);
         if (dx0 != dx) range(dx0, (size_t)T * in * 2, false);

@@ -59,6 +59,7 @@ def test_forward_argument_errors(bd):
     assert call(y=A + 16) == 8 and call(y=2 * A) == 8 and call(y=5 * A + 32) == 8          # over x, an A, a B
     assert call(y=7 * A + 16) == 8                                                          # over y0, but not y0 itself
     assert call(h=8 * A) == 8 and call(h=7 * A + 16) == 8 and call(h=A) == 8 and call(h=4 * A) == 8
+    assert call(y=6 * A) == 8 and call(h=6 * A + 4) == 8                                    # over the scales
     assert call(T=0, x=0, a=None, y=0) == 0
     # only tenants with tokens count: the other's rank and pointers are not looked at, and what is not needed may be missing
     assert call(r=_i32(999, 8), a=_ptrs(None, None), tok=_i32(1, 1, 1)) == 1
@@ -104,6 +105,7 @@ def test_backward_argument_errors(bd):
     assert call(dx=A) == 8 and call(dx=2 * A + 32) == 8 and call(dx=9 * A + 16) == 8 and call(dx=4 * A) == 8 and call(dx=6 * A) == 8
     assert call(da=_ptrs(11 * A, 11 * A)) == 8 and call(da=_ptrs(11 * A, 11 * A + 16 * 64 * 4 - 16)) == 8 and call(db=_ptrs(11 * A, 14 * A)) == 8
     assert call(da=_ptrs(10 * A, 12 * A)) == 8 and call(da=_ptrs(3 * A, 12 * A)) == 8 and call(db=_ptrs(2 * A, 14 * A)) == 8
+    assert call(dx=8 * A) == 8 and call(da=_ptrs(8 * A + 4, 12 * A)) == 8                   # over the scales
     # the gradients of a tenant without a token are checked too: they are set to zero
     one = _i32(1, 1, 1)
     assert call(tok=one, da=_ptrs(12 * A, 12 * A)) == 8 and call(tok=one, r=_i32(300, 8)) == 2 and call(tok=one, da=_ptrs(11 * A + 2, 12 * A)) == 3
