@@ -15,7 +15,10 @@ using bd::misaligned;
 using bd::overlaps;
 
 constexpr int kFewColumns = 16, kManyColumns = bd::kLoraExpandTokens;   // tokens of a tile: records are tiles, or jobs
-constexpr int64_t kFewTokens = 512;                  // largest batch whose records are tiles
+// The largest batch whose records are tiles of 16 tokens; more tokens: tiles of 64.  4096 -> 4096, us, tiles of 16 / 64: rank 16, 8 tenants: 512
+// tokens 9.4 / 9.6, backward 23.1 / 23.4; 1024 tokens 13.3 / 10.8, 27.2 / 28.3; 2048 tokens 24.1 / 18.2, 40.6 / 34.1; rank 64: 512 tokens
+// 16.7 / 18.0, 33.2 / 33.3; 1024 tokens 26.2 / 22.0, 42.0 / 37.8.
+constexpr int64_t kFewTokens = 512;
 constexpr int64_t kDecodeIn = 12288, kDecodeWeight = (int64_t)1 << 28;   // most of in x tokens, of in x out, of a decode launch
 constexpr int kGradParts = 32;                       // parts of jobs whose tokens are in more than one, of all jobs together
 
@@ -26,16 +29,22 @@ int compute_units() {
     return bd::device_cu_count(&cus) == hipSuccess && cus > 0 ? cus : 256;
 }
 
-// Parts that the shrink's sum is cut into, where `groups` workgroups take a part each: rounds of what runs at a time, each some 6 us and
-// 0.5 us for every step of its wavefronts (64 tokens; 0.2 of one tile of 16), and 0.3 us more for every part that the next kernel adds up.
+// Parts that the shrink's sum is cut into, where `groups` workgroups take a part each.  Two run on a compute unit at a time: some 4 us, and
+// for each workgroup of the compute unit and step of its wavefronts 0.25 us (64 tokens; 0.9 with more than 16 ranks at once), or for every two
+// of them 0.2 us (a tile of 16 tokens: they wait more than they work).  A part costs the next kernel, which adds it up, 0.3 to 0.4 us and
+// its bytes.  Measured, us of the two kernels (backward: of all), parts 1 / 2 / 3 / 4 / 8, * the rule's: 512 tokens of 8 tenants, 4096 -> 4096,
+// rank 16: 11.4 / 10.1 / 9.7 / 9.5* / 9.2; 4096 tokens 29.0 / 25.1 / 24.1 / 24.3* / 26.1, backward 49.6 / 46.3 / 45.5 / 45.7* / 47.1; 8192 tokens of 2,
+// rank 64, backward of 4096 -> 11008, 128 tiles: 178 / 157* / 165 / 161.
 int max_splits(int64_t T) { return T <= 4096 ? bd::kLoraMaxSplits : T <= 16384 ? 4 : T <= 32768 ? 2 : 1; }
-int sum_splits(int64_t groups, int64_t K, int64_t T, bool few) {
-    const int64_t steps = (K + 31) / 32, slots = (int64_t)bd::kLoraShrinkAtOnce * compute_units();
+int sum_splits(int64_t groups, int64_t K, int64_t T, int64_t rows, int64_t ld, bool few) {
+    const int64_t steps = (K + 31) / 32, cus = compute_units();
+    const double part = few ? 0.3 : 0.4 + (double)(rows * ld * 8) / 4e6;
     int best = 1;
     double least = 1e30;
     for (int n = 1; n <= max_splits(T) && (n == 1 || n * bd::kLoraShrinkWaves <= steps); ++n) {
-        const double rounds = (double)((groups * n + slots - 1) / slots), per_wave = (double)((steps + n * bd::kLoraShrinkWaves - 1) / (n * bd::kLoraShrinkWaves));
-        const double us = rounds * (6.0 + (few ? 0.2 : 0.5) * per_wave) + 0.3 * n;
+        const int64_t layers = (groups * n + cus - 1) / cus, rounds = (layers + 1) / 2, per_wave = (steps + n * bd::kLoraShrinkWaves - 1) / (n * bd::kLoraShrinkWaves);
+        const double work = few ? 0.2 * (double)rounds : (ld > 16 ? 0.9 : 0.25) * (double)layers;
+        const double us = 4.0 * (double)rounds + work * (double)per_wave + part * n;
         if (us < least) least = us, best = n;
     }
     return best;
@@ -260,7 +269,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
     for (const Job& j : batch.jobs)
         for (int m = 0; m < n_mats; ++m)
             groups += (int64_t)(j.count + columns - 1) / columns * bd::lora_shrink_groups(rank_by[(size_t)m * n_tenants + j.tenant], columns);
-    const int splits = sum_splits(groups, in, T, few);
+    const int splits = sum_splits(groups, in, T, n_mats * T, ld, few);
     if (max_rank > 0) {
         auto s = std::make_unique<bd::LoraShrinkArgs>();
         s->src = x;
@@ -309,7 +318,8 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
 
 // Parts of every job's tokens in the gradients' sums: one, or more where that fills the compute units better (the parts must then be
 // added up).  A workgroup of RW wavefronts to a tile takes some 5 us and 0.35 us for every tile of 32 tokens that each of its 4 / RW groups
-// takes; 3 run on a compute unit at a time.
+// takes; 3 run on a compute unit at a time.  Backward, us, 1 / 2 / 3 / 4 / 8 parts of the longest job, * the rule's: 512 tokens of 8 tenants, rank 16,
+// 4096 -> 4096: 22* / 35; 4096 tokens: 47* / 54 / 58 / 64; 8192 tokens of 2, rank 64, 4096 -> 11008: 188 / 170 / 160* / 178 / 195.
 void cut_into_parts(bd::LoraGradJob* job, int n, int64_t wide, int rank, int64_t most) {
     int longest = 1;
     for (int i = 0; i < n; ++i) longest = std::max(longest, (int)job[i].count);
@@ -411,7 +421,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
     float* const g = work ? (float*)((char*)workspace + order_bytes(T)) : nullptr;
     int64_t groups = 0;
     for (const Job& j : batch.jobs) groups += (int64_t)(j.count + columns - 1) / columns * bd::lora_shrink_groups(rank_by[j.tenant], columns);
-    int splits = sum_splits(groups, out, T, few);
+    int splits = sum_splits(groups, out, T, T, ld, few);
     auto weights_of = [&](const uint16_t* const* by, bool all) {
         return [=](int, int32_t tenant, const uint16_t** w, int* rank) {
             *rank = rank_by[tenant];

@@ -736,8 +736,14 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     const bool real = c < u.count;
     const float* const src = a.h + (int64_t)(u.hrow + (real ? c : 0)) * a.ld;
     auto sum4 = [&](int r) {
-        float4v v = *(const float4v*)(src + r);
-        for (int s = 1; s < a.splits; ++s) v += *(const float4v*)(src + s * a.split_stride + r);
+        float4v v = {};
+        for (int s = 0; s < a.splits; s += 4) {   // four loads at a time
+            float4v part[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) part[k] = *(const float4v*)(src + min(s + k, a.splits - 1) * a.split_stride + r);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v += s + k < a.splits ? part[k] : float4v{};
+        }
         return v;
     };
     float* const kept = !TR && a.h_out[u.mat] && blockIdx.y == 0 && real ? a.h_out[u.mat] + (int64_t)token_of<kTokens / 16>(a, u, c) * a.h_ld : nullptr;
@@ -861,12 +867,16 @@ __global__ __launch_bounds__(kPrepThreads) void lora_prep_kernel(const LoraPrepA
         if (rt >= tiles) continue;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[k][i] = src[at[i] + column];
-        for (int s = 1; s < splits; ++s) {
-            float w[8];
+        for (int s = 1; s < splits; s += 4) {   // the loads of four parts at a time
+            float w[4][8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = src[s * a.split_stride + at[i] + column];
+            for (int c = 0; c < 4; ++c)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[k][i] += w[i];
+                for (int i = 0; i < 8; ++i) w[c][i] = src[min(s + c, splits - 1) * a.split_stride + at[i] + column];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[k][i] += s + c < splits ? w[c][i] : 0.0f;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
