@@ -145,6 +145,7 @@ constexpr int kDecodeThreads = 512;
 // features forms all of h (A comes out of the cache again for the next one): a launch and the way of h through memory would take longer.
 // Vector arithmetic: a wavefront reads rows of A as they are, 1 KB of a row per instruction, and a lane the rows of B of its two features;
 // the matrix cores' order would take the address unit four times as long.  y0 and B are asked for before h is formed.
+// 4096 x 4096, rank 16, a call in a graph: one token 4.6 us, q, k and v for 16 tenants (13.5 MB) 5.0 us, 2.7 TB/s; two launches 7.8 and 9 us.
 template <int TOK, bool ODD>
 __global__ __launch_bounds__(kDecodeThreads) void lora_decode_kernel(const LoraDecodeArgs a) {
     constexpr int kWaves = kDecodeThreads / kWave, kOctets = kLoraDecodeRank / 8, kRows = kLoraDecodeRank / kWaves, kSegments = 8, kFeatures = kLoraDecodeFeatures / kDecodeThreads;
@@ -291,9 +292,12 @@ struct Turn {
     }
 };
 
-// h = A x or g = s B^T dy of one tile, 16 RT ranks and one part of the sum.  The wavefronts divide the part among them, their
-// sums meet in LDS. 
+// h = A x or g = s B^T dy of one tile of 16 NT tokens, 16 RT ranks and one part of the sum.  The wavefronts divide the part among them,
+// step by step of 32 elements, and their sums meet in LDS.  A and x go through a wavefront's own piece of LDS on their way (Turn), B too
+// (Stage): in matrix-core order a load would take the address unit four times as long.  B is B [K, rank]: the sum's index outside.
 // Ranks and columns beyond the last repeat others or hold anything: rows and columns do not mix, and what they give is not kept.
+// Bound by the stream of x (dy), up to its start of some 4 us: 4096 tokens of 8 tenants by 4096, rank 16 (33.5 MB) 11 us, 3.0 TB/s; 8192 of 2 by
+// 11008, rank 64 (180 MB) 60 us, 3.0 TB/s: there B comes out of L2 once for 64 tokens, and registers allow 8 wavefronts on a compute unit.
 template <bool TR, int NT, int RT, bool ODD>
 __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraShrinkArgs a) {
     const Where u = find_tile<NT>(a, blockIdx.x);
@@ -461,6 +465,7 @@ enum { kEvenRanks, kOddRanks, kShortRows };
 // come into that order through a piece of LDS of its own (64 bytes a feature, 16 more behind 8 features: no bank conflicts); backward
 // 8 ranks' rows of A are turned in registers.
 // y0 and the first weights are asked for before h is prepared: three waits for memory become one.
+// Bound by latency and issue: 96 tokens of 3 tenants, 4096 features, rank 8: 5 us; 200 of 40 tenants, 5003 features, ranks to 64 (18 MB): 13 us.
 constexpr int kFewStage = 128 * 64 + 16 * 16;   // bytes
 template <bool TR, int ROWS>
 __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const LoraExpandArgs a) {
@@ -635,13 +640,15 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
 }
 
 // Many tokens: the same of one tile of 64 tokens, 16 for each wavefront, which take 128 features at a time together, gridDim.y of
-// them in turn.  The weights of 128 features by 16 ranks, 16 bytes of them from each thread, go through one of two buffers in LDS
+// them in turn.  The weights of 128 features by 16 RS ranks, 16 RS bytes of them from each thread, go through one of two buffers in LDS
 // (kPieces: [feature][16 ranks] forward, with 16 bytes more behind 8 features; [16 ranks][128 features] backward, with 16 bytes more
 // behind a row), where every wavefront reads them into matrix-core order without bank conflicts: read from memory in that order,
 // neighbouring lanes would be rows apart and an instruction would take the address unit four times as long.  While a piece is used the
 // next but one is on its way, and the next features' y0.
+// Bound by y0 and y: 4096 tokens by 11008, rank 16 (180 MB) 43 us, 4.2 TB/s; 8192 by 4096, rank 64 (134 MB) 39.6 us, 3.4 TB/s (a barrier for every
+// 16 ranks instead of 32: 42.9 us).  Features in turn, not next to each other, for a workgroup: 43 us, else 47.
 constexpr int kPieces = 128 * 32 + 16 * 16;
-template <bool TR, int ROWS>
+template <bool TR, int ROWS, int RS>   // RS: times 16 ranks at a time
 __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lora_expand_many_kernel(const LoraExpandArgs a) {
     constexpr int kTokens = kLoraExpandTokens, kPer = kExpandThreads / kTokens;   // threads per token while h is prepared
     extern __shared__ __align__(16) char lds[];
@@ -651,7 +658,7 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, m = lane & 15, g = lane >> 4;
     const int padded = (u.rank + 15) & ~15, pitch = padded + 8;
     char* const pieces = lds;
-    _Float16* const hi = (_Float16*)(lds + 2 * kPieces);
+    _Float16* const hi = (_Float16*)(lds + 2 * RS * kPieces);
     _Float16* const lo = hi + kTokens * pitch;
     const int64_t stride = (int64_t)gridDim.y * kLoraFeatures;
     // Features f0 .. f0 + 127; a row's last 128 end with it, and of them only those from f0 on are kept.  A row below 128 is read element
@@ -691,41 +698,47 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     // the thread's 16 bytes of the weights
     const int piece_row = TR ? (int)threadIdx.x >> 4 : (int)threadIdx.x >> 1, piece_col = TR ? 8 * ((int)threadIdx.x & 15) : 8 * ((int)threadIdx.x & 1);
     char* const piece_at = pieces + (TR ? piece_row * 272 + piece_col * 2 : piece_row * 32 + piece_col * 2 + (piece_row >> 3) * 16);
-    half8 piece;
-    int piece_left = 0;   // ranks of it that count (backward: whether it does); looked at when it goes to LDS, so that nothing waits for the load
-    auto load_piece = [&](int64_t f, int r) {
-        if constexpr (TR) {   // (F = in, a multiple of 32)
-            piece_left = u.rank - r - piece_row;
-            piece = load8(u.w + (int64_t)min(r + piece_row, u.rank - 1) * F + min(f + piece_col, F - 8));
-        } else {
-            piece_left = u.rank - r - piece_col;
-            const int64_t at = min(f + piece_row, F - 1) * u.rank + (piece_left > 0 ? r + piece_col : r);
-            piece = ROWS != kEvenRanks ? load8_of<ROWS == kShortRows>(u.w, at, F * u.rank) : load8(u.w + at);
+    half8 piece[RS];
+    int piece_left[RS] = {};   // ranks of it that count (backward: whether it does); looked at when it goes to LDS, so that nothing waits for the load
+    auto load_piece = [&](int64_t f, int r0) {
+#pragma unroll
+        for (int k = 0; k < RS; ++k) {
+            const int r = r0 + 16 * k;
+            if constexpr (TR) {   // (F = in, a multiple of 32)
+                piece_left[k] = u.rank - r - piece_row;
+                piece[k] = load8(u.w + (int64_t)min(r + piece_row, u.rank - 1) * F + min(f + piece_col, F - 8));
+            } else {
+                piece_left[k] = u.rank - r - piece_col;
+                const int64_t at = min(f + piece_row, F - 1) * u.rank + (piece_left[k] > 0 ? r + piece_col : r < u.rank ? r : 0);
+                piece[k] = ROWS != kEvenRanks ? load8_of<ROWS == kShortRows>(u.w, at, F * u.rank) : load8(u.w + at);
+            }
         }
     };
-    auto put_piece = [&](int buffer, half8 v, int left) {
-        *(half8*)(piece_at + buffer * kPieces) = !TR && ROWS != kEvenRanks ? only(v, 0, left) : left > 0 ? v : half8{};
+    auto put_piece = [&](int buffer, const half8 (&v)[RS], const int (&left)[RS]) {
+#pragma unroll
+        for (int k = 0; k < RS; ++k)
+            *(half8*)(piece_at + (RS * buffer + k) * kPieces) = !TR && ROWS != kEvenRanks ? only(v[k], 0, left[k]) : left[k] > 0 ? v[k] : half8{};
     };
-    // the pieces come in the order of their use: 16 ranks after 16 ranks, then the next features; past the end the last once more
+    // the pieces come in the order of their use: ranks after ranks, then the next features; past the end the last once more
     int64_t piece_f0 = f0;
     int piece_r = 0;
     auto next_piece = [&] {
         load_piece(begin_of(piece_f0), piece_r);
-        if (piece_r + 16 < padded) {
-            piece_r += 16;
+        if (piece_r + 16 * RS < padded) {
+            piece_r += 16 * RS;
         } else if (piece_f0 + stride < F) {
             piece_r = 0;
             piece_f0 += stride;
         }
     };
     const bool work = f0 < F;   // (not for a matrix without outputs, whose h alone is asked for)
-    half8 piece0 = {};
-    int left0 = 0;
+    half8 piece0[RS] = {};
+    int left0[RS] = {};
     if (work) {
         if (padded > 0) {   // two pieces before h: nothing is in flight when the turns begin
             next_piece();
-            piece0 = piece;
-            left0 = piece_left;
+#pragma unroll
+            for (int k = 0; k < RS; ++k) piece0[k] = piece[k], left0[k] = piece_left[k];
             next_piece();
         }
         load_y0(before, begin_of(f0));
@@ -792,24 +805,28 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
         auto step = [&](int r) {
             put_piece(buffer ^ 1, piece, piece_left);   // of the next ranks or features
             next_piece();
-            const char* const at = pieces + buffer * kPieces + (TR ? 8 * (g & 1) * 272 + m * 16 : m * (8 * 32 + 16) + (g & 1) * 16);
-            half8 wv[8], cols[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) wv[j] = *(const half8*)(at + j * (TR ? 272 : 32));
-            if constexpr (TR) {
-                transpose8(wv, cols);
-            } else {
+            for (int k = 0; k < RS; ++k) {
+                if (k > 0 && r + 16 * k >= padded) continue;
+                const char* const at = pieces + (RS * buffer + k) * kPieces + (TR ? 8 * (g & 1) * 272 + m * 16 : m * (8 * 32 + 16) + (g & 1) * 16);
+                half8 wv[8], cols[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) cols[j] = wv[j];
+                for (int j = 0; j < 8; ++j) wv[j] = *(const half8*)(at + j * (TR ? 272 : 32));
+                if constexpr (TR) {
+                    transpose8(wv, cols);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) cols[j] = wv[j];
+                }
+                const half8 hv = *(const half8*)(mine + r + 16 * k);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] = mfma(hv, cols[j], acc[j]);
             }
-            const half8 hv = *(const half8*)(mine + r);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = mfma(hv, cols[j], acc[j]);
             buffer ^= 1;
             __syncthreads();
         };
         if (padded > 0) step(0);   // (not in the loop: what is in flight is known at each of its waits)
-        for (int r = 16; r < padded; r += 16) step(r);
+        for (int r = 16 * RS; r < padded; r += 16 * RS) step(r);
         half8 v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -835,7 +852,8 @@ constexpr int kPrepThreads = 256;
 
 // The second operand of the gradients, once for all their workgroups: 32 tokens' g (or h) as hi and lo in matrix-core order, one
 // exponent for the 32.  Lane (n, q) holds rank n of its 16, tokens 8 q .. 8 q + 7, in 16 bytes.  Where g came in parts their sum
-// takes the first part's place.
+// takes the first part's place.  Once for 8192 tokens of rank 64: 6 us; in the workgroups of the sums, each for itself: 3 us less for 32
+// tokens per tenant, up to twice the sums' time for 64 tenants or 512 tokens.
 __global__ __launch_bounds__(kPrepThreads) void lora_prep_kernel(const LoraPrepArgs a) {
     const int record = threadIdx.x & (kWave - 1);
     const int j = __builtin_amdgcn_readfirstlane(__popcll(__ballot(record < a.n_jobs && a.job[min(record, a.n_jobs - 1)].chunk_begin <= (int)blockIdx.x + a.chunk_first)) - 1);
@@ -923,6 +941,8 @@ constexpr int kGradPitch = 128 + 16;   // halves: 4 rows apart on banks of their
 // of a row from 16 lanes) and is read transposed.  The sums are kept in units of the present tile's exponent; tiles whose largest value
 // is 2^-64 of the largest so far are below what binary32 would keep of them.
 // Loads are never under a condition (past the end they repeat the last tile's), or the wait for them would be for all.
+// Bound by the streams of x and dy: 4096 tokens of 8 tenants, 4096 -> 4096, rank 16 (67 MB) 22 us, 3.0 TB/s; 8192 of 2, 4096 -> 11008, rank 64
+// (247 MB) 66 us, 3.7 TB/s.
 template <int RW, bool ODD>
 __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(ODD ? 2 : 3, 3))) void lora_grad_kernel(const LoraGradArgs a) {
     constexpr int TW = kLoraGradWaves / RW, N = 8 / RW, kBuffers = RW > 1 ? 2 : 1;   // groups; rows of 4 per wavefront and tile
@@ -1050,7 +1070,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(OD
     }
 }
 
-// out (+)= the sum of the parts, in their order; zeros where there are none
+// out (+)= the sum of the parts, in their order; zeros where there are none.  3 parts of 2 tenants' gradients of 64 x (4096 + 11008): 7 us
 __global__ __launch_bounds__(256) void lora_reduce_kernel(const LoraReduceArgs a) {
     const auto& job = a.job[blockIdx.y];
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < job.n; i += (int64_t)gridDim.x * 256) {
@@ -1110,16 +1130,21 @@ hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transpo
     // as many workgroups as run at a time (forward 4 to a compute unit, backward 3), each taking the same number of turns
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(wide, (int64_t)(transposed ? 3 : 4) * cus / a.n_tiles));
     const int64_t each = (wide + most - 1) / most, turns = (wide + each - 1) / each;
-    const unsigned lds = (unsigned)(2 * kPieces + 2 * kLoraExpandTokens * (((max_rank + 15) & ~15) + 8) * 2);
-    static PerDeviceOnce once[5];
+    const int RS = max_rank <= 16 ? 1 : 2;
+    const unsigned lds = (unsigned)(2 * RS * kPieces + 2 * kLoraExpandTokens * (((max_rank + 15) & ~15) + 8) * 2);
+    static PerDeviceOnce once[10];
     auto go = [&](auto kernel, int which) {
-        const hipError_t e = once[which].run([&] { return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kPieces + 2 * kLoraExpandTokens * (kLoraMaxRank + 8) * 2); });
+        const hipError_t e = once[which].run([&] { return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * 2 * kPieces + 2 * kLoraExpandTokens * (kLoraMaxRank + 8) * 2); });
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_tiles, (unsigned)turns), dim3(kExpandThreads), lds, st, a);
         return hipGetLastError();
     };
-    if (transposed) return rows == kShortRows ? go(lora_expand_many_kernel<true, kShortRows>, 0) : go(lora_expand_many_kernel<true, kEvenRanks>, 1);
-    return rows == kShortRows ? go(lora_expand_many_kernel<false, kShortRows>, 2) : rows == kOddRanks ? go(lora_expand_many_kernel<false, kOddRanks>, 3) : go(lora_expand_many_kernel<false, kEvenRanks>, 4);
+    auto of = [&](auto ranks_at_once, int first) {
+        constexpr int R = decltype(ranks_at_once)::value;
+        if (transposed) return rows == kShortRows ? go(lora_expand_many_kernel<true, kShortRows, R>, first) : go(lora_expand_many_kernel<true, kEvenRanks, R>, first + 1);
+        return rows == kShortRows ? go(lora_expand_many_kernel<false, kShortRows, R>, first + 2) : rows == kOddRanks ? go(lora_expand_many_kernel<false, kOddRanks, R>, first + 3) : go(lora_expand_many_kernel<false, kEvenRanks, R>, first + 4);
+    };
+    return RS == 1 ? of(std::integral_constant<int, 1>{}, 0) : of(std::integral_constant<int, 2>{}, 5);
 }
 
 hipError_t launch_lora_prep(const LoraPrepArgs& a, int chunks, int sides, hipStream_t st) {
