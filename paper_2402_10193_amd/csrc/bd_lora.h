@@ -83,6 +83,16 @@ struct LoraExpandArgs {
     };
 };
 
+// order[position among the tokens sorted by job] = token, for `count` tokens from `first` on: their jobs, `bits` each, and where the next token of
+// every job goes
+constexpr int kLoraOrderJobs = 256, kLoraOrderBytes = 2944;
+struct LoraOrderArgs {
+    int32_t* order;
+    int32_t first, count, bits, n_jobs;
+    int32_t begin[kLoraOrderJobs];
+    uint8_t job[kLoraOrderBytes];
+};
+
 struct LoraDecodeArgs {
     const uint16_t* x;                  // [T, in]
     const uint16_t* y0[kLoraMaxMats];   // may be nullptr
@@ -147,6 +157,7 @@ constexpr int lora_shrink_groups(int rank, int columns) { return (rank + 15) / 1
 
 // `columns`: tokens of a tile (16: records are tiles; else records are jobs, 64).  max_rank: the largest rank of the records;
 // odd: some rank is not a multiple of 8 (B's rows are then no whole 16-byte pieces).
+hipError_t launch_lora_order(const LoraOrderArgs& a, hipStream_t st);
 hipError_t launch_lora_decode(const LoraDecodeArgs& a, int max_tokens, int64_t max_F, bool odd, hipStream_t st);
 hipError_t launch_lora_shrink(const LoraShrinkArgs& a, int columns, bool transposed, int max_rank, bool odd, hipStream_t st);
 hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transposed, int max_rank, int64_t min_F, int64_t max_F, bool odd, hipStream_t st);

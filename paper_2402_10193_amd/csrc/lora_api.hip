@@ -71,6 +71,36 @@ Batch group(const int32_t* tenant_of_token, int64_t T, int32_t n_tenants) {
     return b;
 }
 
+// The order of the tokens into device memory: by the tokens' jobs, which the device sorts, where that takes fewer launches than the order itself
+// (bd::write_int_table: a few runs, or 960 tokens a launch).
+hipError_t write_order(const Batch& b, int64_t T, int32_t* dst, hipStream_t st) {
+    const int n = (int)std::min<size_t>(b.jobs.size(), bd::kLoraOrderJobs + 1);
+    const int bits = n <= 2 ? 1 : n <= 4 ? 2 : n <= 16 ? 4 : 8;
+    const int64_t each = bd::kLoraOrderBytes * 8 / bits;
+    int64_t runs = 1;
+    for (size_t i = 1; i < b.order.size(); ++i) runs += b.order[i] != b.order[i - 1] + 1;
+    const int64_t launches = std::min((runs + 319) / 320, (T + 959) / 960);
+    if (n > bd::kLoraOrderJobs || (T + each - 1) / each >= launches) return bd::write_int_table(b.order, dst, st);
+    std::vector<uint8_t> job((size_t)T);
+    auto a = std::make_unique<bd::LoraOrderArgs>();
+    for (int j = 0; j < n; ++j) {
+        a->begin[j] = b.jobs[(size_t)j].first;
+        for (int32_t i = 0; i < b.jobs[(size_t)j].count; ++i) job[(size_t)b.order[(size_t)(b.jobs[(size_t)j].first + i)]] = (uint8_t)j;
+    }
+    a->order = dst;
+    a->bits = bits;
+    a->n_jobs = n;
+    for (int64_t first = 0; first < T; first += each) {
+        a->first = (int32_t)first;
+        a->count = (int32_t)std::min(each, T - first);
+        std::memset(a->job, 0, sizeof(a->job));
+        for (int32_t i = 0; i < a->count; ++i) a->job[i * bits >> 3] |= (uint8_t)(job[(size_t)(first + i)] << (i * bits & 7));
+        if (const hipError_t e = bd::launch_lora_order(*a, st); e != hipSuccess) return e;
+        for (int32_t i = 0; i < a->count; ++i) ++a->begin[job[(size_t)(first + i)]];
+    }
+    return hipSuccess;
+}
+
 // Fills the records of one kernel's launches and runs them: `per_record` says whether a (job, matrix) takes part, with which
 // weight and rank.
 template <typename Args, typename Weight, typename Launch>
@@ -260,7 +290,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
     const int columns = few ? kFewColumns : kManyColumns;
     const int32_t* order = nullptr;
     if (!few && !batch.order.empty() && max_rank > 0) {
-        if (bd::write_int_table(batch.order, (int32_t*)workspace, st) != hipSuccess) return BD_ERR_DEVICE;
+        if (write_order(batch, T, (int32_t*)workspace, st) != hipSuccess) return BD_ERR_DEVICE;
         order = (const int32_t*)workspace;
     }
     float* const hw = (float*)((char*)workspace + order_bytes(T));
@@ -415,7 +445,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
     const int64_t ld = round_up(max_rank, 16);
     const int32_t* order = nullptr;
     if (work && !batch.order.empty()) {   // (the gradients' sums run over a job's tokens, for few tokens too)
-        if (bd::write_int_table(batch.order, (int32_t*)workspace, st) != hipSuccess) return BD_ERR_DEVICE;
+        if (write_order(batch, T, (int32_t*)workspace, st) != hipSuccess) return BD_ERR_DEVICE;
         order = (const int32_t*)workspace;
     }
     float* const g = work ? (float*)((char*)workspace + order_bytes(T)) : nullptr;

@@ -139,6 +139,50 @@ __device__ __forceinline__ void tokens_of(const Args& a, const Where& u, const i
     }
 }
 
+constexpr int kOrderThreads = 1024;
+
+// The stable sort of tokens by job, one workgroup: a wavefront counts its run of tokens by job, the counts become places, and it goes through the
+// run again, 64 tokens at a time: a token's place among the 64 from one vote per bit of the job.  4756 tokens of 5 jobs: 5 us, where their
+// order itself, 960 tokens to a launch's arguments, takes 5 launches of 3 us.
+__global__ __launch_bounds__(kOrderThreads) void lora_order_kernel(const LoraOrderArgs a) {
+    constexpr int kWaves = kOrderThreads / kWave;
+    __shared__ int place[kWaves][kLoraOrderJobs];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int each = (a.count + kOrderThreads - 1) / kOrderThreads * kWave, begin = min(wave * each, a.count), end = min(begin + each, a.count);
+    auto job_of = [&](int i) { return (a.job[i * a.bits >> 3] >> (i * a.bits & 7)) & ((1 << a.bits) - 1); };
+    for (int j = threadIdx.x; j < kWaves * kLoraOrderJobs; j += kOrderThreads) (&place[0][0])[j] = 0;
+    __syncthreads();
+    for (int i = begin + lane; i < end; i += kWave) atomicAdd(&place[wave][job_of(i)], 1);
+    __syncthreads();
+    if ((int)threadIdx.x < a.n_jobs) {
+        int at = a.begin[threadIdx.x];
+        for (int w = 0; w < kWaves; ++w) {
+            const int n = place[w][threadIdx.x];
+            place[w][threadIdx.x] = at;
+            at += n;
+        }
+    }
+    __syncthreads();
+    for (int i0 = begin; i0 < end; i0 += kWave) {
+        const int i = i0 + lane;
+        const bool real = i < end;
+        const int job = real ? job_of(i) : 0;
+        uint64_t same = __ballot(real);
+        for (int k = 0; k < a.bits; ++k) {
+            const uint64_t set = __ballot((job >> k) & 1);
+            same &= (job >> k) & 1 ? set : ~set;
+        }
+        const int before = __popcll(same & ((1ull << lane) - 1));
+        const int at = place[wave][job];
+        __builtin_amdgcn_wave_barrier();
+        if (real) {
+            a.order[at + before] = a.first + i;
+            if (before == 0) place[wave][job] = at + __popcll(same);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
 constexpr int kDecodeThreads = 512;
 
 // A decode step: up to 2 tokens of a tenant, up to 16 ranks, both products in one launch, bound by latency.  Every workgroup of 1024
@@ -1082,8 +1126,15 @@ __global__ __launch_bounds__(256) void lora_reduce_kernel(const LoraReduceArgs a
 
 }  // namespace
 
-static_assert(sizeof(LoraDecodeArgs) <= 4096 && sizeof(LoraShrinkArgs) <= 4096 && sizeof(LoraExpandArgs) <= 4096 && sizeof(LoraGradArgs) <= 4096 && sizeof(LoraReduceArgs) <= 4096 && sizeof(LoraPrepArgs) <= 4096,
+static_assert(sizeof(LoraOrderArgs) <= 4096 && sizeof(LoraDecodeArgs) <= 4096 && sizeof(LoraShrinkArgs) <= 4096 && sizeof(LoraExpandArgs) <= 4096 && sizeof(LoraGradArgs) <= 4096 && sizeof(LoraReduceArgs) <= 4096 && sizeof(LoraPrepArgs) <= 4096,
               "kernel arguments");
+
+hipError_t launch_lora_order(const LoraOrderArgs& a, hipStream_t st) {
+    if (a.count < 1 || a.n_jobs < 1 || a.n_jobs > kLoraOrderJobs || (a.bits != 1 && a.bits != 2 && a.bits != 4 && a.bits != 8) || a.n_jobs > 1 << a.bits || a.count > kLoraOrderBytes * 8 / a.bits)
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL(lora_order_kernel, dim3(1), dim3(kOrderThreads), 0, st, a);
+    return hipGetLastError();
+}
 
 hipError_t launch_lora_decode(const LoraDecodeArgs& a, int max_tokens, int64_t max_F, bool odd, hipStream_t st) {
     const int64_t groups = max_F > 0 ? (max_F + kLoraDecodeFeatures - 1) / kLoraDecodeFeatures : 1;   // (F = 0: h alone)

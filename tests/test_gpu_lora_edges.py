@@ -92,3 +92,34 @@ def test_many_tenants_of_few_tokens(bd, ranks, per_tenant):
         ref64.check(h[rows, :ranks[e]], want_h, (inn / 8 + 16) * ref64.U32 * size, f"h of tenant {e}")
     for t, e in enumerate(tok):
         assert (h[t, ranks[e]:] == 7.0).all()
+
+
+@pytest.mark.parametrize("T,n", [(2000, 2), (9000, 3), (7000, 10), (13000, 16), (6000, 200), (3000, 256), (3000, 257), (24000, 2)])
+def test_order_of_many_mixed_tokens(bd, T, n):
+    """Tokens of every number of tenants in any order, on both sides of what one launch sorts: the same bits as of the tokens grouped by tenant."""
+    gen = torch.Generator().manual_seed(8)
+    out, inn = 136, 64
+    a, b = _adapters([4] * n, out, inn, gen)
+    table = bd.LoraTable(a, b, torch.rand(n, generator=gen))
+    tok = torch.randint(0, n, (T,), generator=gen, dtype=torch.int32)
+    tok[:n] = torch.arange(n, dtype=torch.int32)
+    order = torch.sort(tok, stable=True).indices
+    x = torch.randn(T, inn, generator=gen).half().to(DEV)
+    dy = torch.randn(T, out, generator=gen).half().to(DEV)
+    here = order.to(DEV)
+    grads = lambda: ([torch.empty(4, inn, device=DEV) for _ in range(n)], [torch.empty(out, 4, device=DEV) for _ in range(n)])
+    results = []
+    for rows in (None, here):
+        xs, ys, ts = (x, dy, tok) if rows is None else (x[rows].contiguous(), dy[rows].contiguous(), tok[order])
+        h = torch.empty(T, 4, device=DEV)
+        y = bd.lora_multitenant(xs, table, ts, y0=ys, h=h)
+        g = grads()
+        dx = bd.lora_multitenant_backward(ys, xs, h, table, ts, bd.LoraGrads(table, *g), dx0=xs)
+        results.append((y, h, dx, *g))
+    (y, h, dx, da, db), (y2, h2, dx2, da2, db2) = results
+    assert torch.equal(y[here], y2) and torch.equal(h[here], h2) and torch.equal(dx[here], dx2)
+    assert all(torch.equal(p, q) for p, q in zip(da + db, da2 + db2))
+    e = int(tok[5])
+    rows = (tok == e).nonzero()[:, 0].to(DEV)
+    want, _, bound = ref64.forward(x[rows], a, b, table.scale, [e] * len(rows), dy[rows], out)
+    ref64.check(y[rows], want, bound, "y")
