@@ -32,13 +32,13 @@ int compute_units() {
 // Parts that the shrink's sum is cut into, where `groups` workgroups take a part each.  Two run on a compute unit at a time: some 4 us, and
 // for each workgroup of the compute unit and step of its wavefronts 0.25 us (64 tokens; 0.9 with more than 16 ranks at once), or for every two
 // of them 0.2 us (a tile of 16 tokens: they wait more than they work).  A part costs the next kernel, which adds it up, 0.3 to 0.4 us and
-// its bytes.  Measured, us of the two kernels (backward: of all), parts 1 / 2 / 3 / 4 / 8, * the rule's: 512 tokens of 8 tenants, 4096 -> 4096,
+// its bytes, and `again` rows out of the caches where all of its workgroups read their tile's.  Measured, us of the two kernels (backward: of all), parts 1 / 2 / 3 / 4 / 8, * the rule's: 512 tokens of 8 tenants, 4096 -> 4096,
 // rank 16: 11.4 / 10.1 / 9.7 / 9.5* / 9.2; 4096 tokens 29.0 / 25.1 / 24.1 / 24.3* / 26.1, backward 49.6 / 46.3 / 45.5 / 45.7* / 47.1; 8192 tokens of 2,
 // rank 64, backward of 4096 -> 11008, 128 tiles: 178 / 157* / 165 / 161.
 int max_splits(int64_t T) { return T <= 4096 ? bd::kLoraMaxSplits : T <= 16384 ? 4 : T <= 32768 ? 2 : 1; }
-int sum_splits(int64_t groups, int64_t K, int64_t T, int64_t rows, int64_t ld, bool few) {
+int sum_splits(int64_t groups, int64_t K, int64_t T, int64_t rows, int64_t ld, bool few, int64_t again) {
     const int64_t steps = (K + 31) / 32, cus = compute_units();
-    const double part = few ? 0.3 : 0.4 + (double)(rows * ld * 8) / 4e6;
+    const double part = (few ? 0.3 : 0.4 + (double)(rows * ld * 8) / 4e6) + (double)(again * ld * 4) / 1e7;
     int best = 1;
     double least = 1e30;
     for (int n = 1; n <= max_splits(T) && (n == 1 || n * bd::kLoraShrinkWaves <= steps); ++n) {
@@ -69,6 +69,14 @@ Batch group(const int32_t* tenant_of_token, int64_t T, int32_t n_tenants) {
         ++b.jobs.back().count;
     }
     return b;
+}
+
+// Rows of h that the workgroups of the second product read: their tile's each (4 to a compute unit at most).
+int64_t rows_again(const Batch& b, int64_t F, int columns) {
+    int64_t tiles = 0;
+    for (const Job& j : b.jobs) tiles += (j.count + columns - 1) / columns;
+    const int64_t wide = (F + bd::kLoraFeatures - 1) / bd::kLoraFeatures;
+    return columns == kFewColumns ? tiles * (wide + 3) / 4 * columns : std::min<int64_t>(4 * compute_units(), tiles * wide) * columns;
 }
 
 // The order of the tokens into device memory: by the tokens' jobs, which the device sorts, where that takes fewer launches than the order itself
@@ -299,7 +307,7 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
     for (const Job& j : batch.jobs)
         for (int m = 0; m < n_mats; ++m)
             groups += (int64_t)(j.count + columns - 1) / columns * bd::lora_shrink_groups(rank_by[(size_t)m * n_tenants + j.tenant], columns);
-    const int splits = sum_splits(groups, in, T, n_mats * T, ld, few);
+    const int splits = sum_splits(groups, in, T, n_mats * T, ld, few, rows_again(batch, max_out, columns) * n_mats);
     if (max_rank > 0) {
         auto s = std::make_unique<bd::LoraShrinkArgs>();
         s->src = x;
@@ -451,7 +459,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
     float* const g = work ? (float*)((char*)workspace + order_bytes(T)) : nullptr;
     int64_t groups = 0;
     for (const Job& j : batch.jobs) groups += (int64_t)(j.count + columns - 1) / columns * bd::lora_shrink_groups(rank_by[j.tenant], columns);
-    int splits = sum_splits(groups, out, T, T, ld, few);
+    int splits = sum_splits(groups, out, T, T, ld, few, any_da || any_db ? 0 : rows_again(batch, in, columns));
     auto weights_of = [&](const uint16_t* const* by, bool all) {
         return [=](int, int32_t tenant, const uint16_t** w, int* rank) {
             *rank = rank_by[tenant];
