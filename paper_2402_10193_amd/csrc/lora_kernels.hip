@@ -792,27 +792,39 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     const int c = threadIdx.x / kPer, sub = threadIdx.x % kPer;
     const bool real = c < u.count;
     const float* const src = a.h + (int64_t)(u.hrow + (real ? c : 0)) * a.ld;
-    auto sum4 = [&](int r) {
-        float4v v = {};
-        for (int s = 0; s < a.splits; s += 4) {   // four loads at a time
-            float4v part[4];
+    // HELD times four ranks of the thread at a time, 4 sub + 16 k behind r, two parts of each: all their loads before the first addition
+    constexpr int kHeld = RS == 1 ? 1 : 4;
+    auto sums = [&](int r, float4v (&v)[kHeld]) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) part[k] = *(const float4v*)(src + min(s + k, a.splits - 1) * a.split_stride + r);
+        for (int k = 0; k < kHeld; ++k) v[k] = float4v{};
+        constexpr int kAtOnce = RS == 1 ? 4 : 2;
+        for (int s = 0; s < a.splits; s += kAtOnce) {
+            float4v part[kAtOnce][kHeld];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v += s + k < a.splits ? part[k] : float4v{};
+            for (int c = 0; c < kAtOnce; ++c)
+#pragma unroll
+                for (int k = 0; k < kHeld; ++k) part[c][k] = *(const float4v*)(src + min(s + c, a.splits - 1) * a.split_stride + min(r + 16 * k, padded - 16) + 4 * sub);
+#pragma unroll
+            for (int c = 0; c < kAtOnce; ++c)
+#pragma unroll
+                for (int k = 0; k < kHeld; ++k) v[k] += s + c < a.splits ? part[c][k] : float4v{};
         }
-        return v;
     };
     float* const kept = !TR && a.h_out[u.mat] && blockIdx.y == 0 && real ? a.h_out[u.mat] + (int64_t)token_of<kTokens / 16>(a, u, c) * a.h_ld : nullptr;
     float top = 0.0f;
-    float4v first = {};   // of the thread's first four ranks: all there are of 16
-    for (int r = 4 * sub; r < padded; r += 4 * kPer) {
-        const float4v v = sum4(r);
-        if (r == 4 * sub) first = v;
+    float4v first[kHeld];   // of the thread's first ranks: all there are up to 16 (RS = 1) or 64
+    for (int r = 0; r < padded; r += 16 * kHeld) {
+        float4v v[kHeld];
+        sums(r, v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            top = fmaxf(top, finite_abs(v[i]));
-            if (kept && r + i < u.rank) kept[r + i] = v[i];
+        for (int k = 0; k < kHeld; ++k) {
+            if (r == 0) first[k] = v[k];
+            if (r + 16 * k >= padded) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                top = fmaxf(top, finite_abs(v[k][i]));
+                if (kept && r + 16 * k + 4 * sub + i < u.rank) kept[r + 16 * k + 4 * sub + i] = v[k][i];
+            }
         }
     }
 #pragma unroll
@@ -820,18 +832,28 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     const int e = group_exponent(top);
     if (sub == 0) unit[c] = power_of_two(e) * scale;
     const float down = power_of_two(-e);
-    for (int r = 4 * sub; r < padded; r += 4 * kPer) {
-        const float4v v = r == 4 * sub ? first : sum4(r);
-        half4 h, l;
+    for (int r = 0; r < padded; r += 16 * kHeld) {
+        float4v v[kHeld];
+        if (r == 0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            _Float16 p, q;
-            split_half(v[i], down, &p, &q);
-            h[i] = real ? p : (_Float16)0.0f;
-            l[i] = real ? q : (_Float16)0.0f;
+            for (int k = 0; k < kHeld; ++k) v[k] = first[k];
+        } else {
+            sums(r, v);
         }
-        *(half4*)(hi + c * pitch + r) = h;
-        *(half4*)(lo + c * pitch + r) = l;
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            if (r + 16 * k >= padded) continue;
+            half4 h, l;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                _Float16 p, q;
+                split_half(v[k][i], down, &p, &q);
+                h[i] = real ? p : (_Float16)0.0f;
+                l[i] = real ? q : (_Float16)0.0f;
+            }
+            *(half4*)(hi + c * pitch + r + 16 * k + 4 * sub) = h;
+            *(half4*)(lo + c * pitch + r + 16 * k + 4 * sub) = l;
+        }
     }
     if (!work) return;   // (of the whole workgroup)
     if (padded > 0) put_piece(0, piece0, left0);
