@@ -71,12 +71,12 @@ Batch group(const int32_t* tenant_of_token, int64_t T, int32_t n_tenants) {
     return b;
 }
 
-// Rows of h that the workgroups of the second product read: their tile's each (4 to a compute unit at most).
+// Rows of h that the workgroups of the second product read: their tile's each (3 to a compute unit at most).
 int64_t rows_again(const Batch& b, int64_t F, int columns) {
     int64_t tiles = 0;
     for (const Job& j : b.jobs) tiles += (j.count + columns - 1) / columns;
     const int64_t wide = (F + bd::kLoraFeatures - 1) / bd::kLoraFeatures;
-    return columns == kFewColumns ? tiles * (wide + 3) / 4 * columns : std::min<int64_t>(4 * compute_units(), tiles * wide) * columns;
+    return columns == kFewColumns ? tiles * (wide + 3) / 4 * columns : std::min<int64_t>(3 * compute_units(), tiles * wide) * columns;
 }
 
 // The order of the tokens into device memory: by the tokens' jobs, which the device sorts, where that takes fewer launches than the order itself

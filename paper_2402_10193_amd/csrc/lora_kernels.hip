@@ -1200,8 +1200,9 @@ hipError_t launch_lora_expand(const LoraExpandArgs& a, int columns, bool transpo
     }
     int cus = 256;
     if (const hipError_t e = device_cu_count(&cus); e != hipSuccess) return e;
-    // as many workgroups as run at a time (forward 4 to a compute unit, backward 3), each taking the same number of turns
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(wide, (int64_t)(transposed ? 3 : 4) * cus / a.n_tiles));
+    // Up to 3 workgroups to a compute unit, each taking the same number of turns.  1 / 2 / 3 / 4 of them, us: 1172 tokens by 5504, rank 64:
+    // 14.9 / 13.7 / 13.6 / 16.6; 4096 by 11008, rank 16: 57 / 47 / 46.6 / 45.8, rank 64: 83 / 56 / 54 / 59; backward, 8192 by 4096, rank 64: 83 / 43 / 39 / 42
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(wide, (int64_t)3 * cus / a.n_tiles));
     const int64_t each = (wide + most - 1) / most, turns = (wide + each - 1) / each;
     const int RS = max_rank <= 16 ? 1 : 2;
     const unsigned lds = (unsigned)(2 * RS * kPieces + 2 * kLoraExpandTokens * (((max_rank + 15) & ~15) + 8) * 2);
