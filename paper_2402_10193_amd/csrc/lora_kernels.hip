@@ -689,7 +689,7 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
 // behind a row), where every wavefront reads them into matrix-core order without bank conflicts: read from memory in that order,
 // neighbouring lanes would be rows apart and an instruction would take the address unit four times as long.  While a piece is used the
 // next but one is on its way, and the next features' y0.
-// Bound by y0 and y: 4096 tokens by 11008, rank 16 (180 MB) 43 us, 4.2 TB/s; 8192 by 4096, rank 64 (134 MB) 39.6 us, 3.4 TB/s (a barrier for every
+// Bound by y0 and y: 4096 tokens by 11008, rank 16 (180 MB) 43 us, 4.2 TB/s; 8192 by 4096, rank 64 (134 MB) 38 us, 3.5 TB/s (a barrier for every
 // 16 ranks instead of 32: 42.9 us).  Features in turn, not next to each other, for a workgroup: 43 us, else 47.
 constexpr int kPieces = 128 * 32 + 16 * 16;
 template <bool TR, int ROWS, int RS>   // RS: times 16 ranks at a time
