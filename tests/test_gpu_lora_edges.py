@@ -123,3 +123,48 @@ def test_order_of_many_mixed_tokens(bd, T, n):
     rows = (tok == e).nonzero()[:, 0].to(DEV)
     want, _, bound = ref64.forward(x[rows], a, b, table.scale, [e] * len(rows), dy[rows], out)
     ref64.check(y[rows], want, bound, "y")
+
+
+@pytest.mark.parametrize("out,inn,T,ranks,mixed", [
+    (40, 64, 700, [40, 129, 256, 1], True), (127, 96, 600, [17, 64], False), (1, 32, 2000, [33], False), (129, 160, 900, [250, 65], True),
+    (1000, 128, 1030, [256, 96], False), (300, 4096, 520, [80, 0, 24], True), (8, 32, 65535, [3, 20, 1], True), (200, 64, 65535, [16], False)])
+def test_ranks_and_rows_of_many_tokens(bd, out, inn, T, ranks, mixed):
+    """Over 16 ranks at once, to the largest; rows below 128 features in and out; the most tokens of a call."""
+    a, b, scale, x, y0 = ref64.make(ranks, out, inn, T, seed=out + T)
+    gen = torch.Generator().manual_seed(9)
+    tok = torch.randint(0, len(ranks), (T,), generator=gen, dtype=torch.int32)
+    tok = (tok if mixed else tok.sort().values).tolist()
+    table = bd.LoraTable(a, b, scale)
+    h = torch.zeros(T, max(ranks), device=DEV)
+    y = bd.lora_multitenant(x, table, tok, y0=y0, h=h)
+    want, h_of, bound = ref64.forward(x, a, b, scale, tok, y0, out)
+    ref64.check(y, want, bound, "y")
+    dy = (torch.randn(T, out, generator=gen) * 0.01).half().to(DEV)
+    dx0 = torch.randn(T, inn, generator=gen).half().to(DEV)
+    da = [torch.empty(r, inn, device=DEV) if r else None for r in ranks]
+    db = [torch.empty(out, r, device=DEV) if r else None for r in ranks]
+    dx = bd.lora_multitenant_backward(dy, x, h, table, tok, bd.LoraGrads(table, da, db), dx0=dx0)
+    want_dx, dx_bound, grads = ref64.backward(dy, x, h, a, b, scale, tok, dx0)
+    ref64.check(dx, want_dx, dx_bound, "dx")
+    for e, (ga, ga_bound, gb, gb_bound) in grads.items():
+        ref64.check(da[e], ga, ga_bound, f"dA of tenant {e}")
+        ref64.check(db[e], gb, gb_bound, f"dB of tenant {e}")
+
+
+@pytest.mark.parametrize("T", [2, 40, 600])
+@pytest.mark.parametrize("rank", [5, 8, 20, 61])
+def test_weights_that_are_not_finite_stay_in_their_row(bd, T, rank):
+    """A row of B reaches its own feature of y alone, a column of A its own feature of dx: all others have the same bits."""
+    out, inn, row, column = 200, 160, 130, 77
+    a, b, scale, x, y0 = ref64.make([rank], out, inn, T, seed=rank)
+    a2, b2 = [a[0].clone()], [b[0].clone()]
+    a2[0][:, column] = float("inf")
+    b2[0][row] = float("nan")
+    table, with_a, with_b = bd.LoraTable(a, b, scale), bd.LoraTable(a2, b, scale), bd.LoraTable(a, b2, scale)
+    tok = [0] * T
+    y, z = (bd.lora_multitenant(x, t, tok, y0=y0) for t in (table, with_b))
+    others = [f for f in range(out) if f != row]
+    assert torch.equal(y[:, others], z[:, others]) and torch.isnan(z[:, row]).all()
+    dx, dz = (bd.lora_multitenant_backward(y0, None, None, t, tok, None, dx0=x) for t in (table, with_a))
+    others = [f for f in range(inn) if f != column]
+    assert torch.equal(dx[:, others], dz[:, others]) and not torch.isfinite(dz[:, column]).any()
