@@ -943,10 +943,7 @@ class LoraTable:
             self.scale = torch.tensor([float(s) for s in scale_by_tenant], dtype=torch.float32, device=dev)
         if self.scale.numel() != len(self.a):
             raise ValueError("one scale per tenant")
-
-    @property
-    def n_tenants(self) -> int:
-        return len(self.a)
+        self.n_tenants, self.device = len(self.a), self.scale.get_device()
 
 
 class LoraGroup:
@@ -969,6 +966,7 @@ class LoraGroup:
         self.b_ptrs = (ctypes.c_void_p * size)(*flat(lambda t: t.b_ptrs))
         self.rank_arr = (ctypes.c_int32 * size)(*flat(lambda t: t.rank_arr))
         self.scales, self.array = [t.scale for t in self.tables], ctypes.c_void_p * self.n
+        self.device = self.tables[0].device if len({t.device for t in self.tables}) == 1 else None
         self.scale = self.array(*[_ptr(t) or None for t in self.scales])
         self.out_arr = (ctypes.c_int64 * self.n)(*self.outs)
 
@@ -987,11 +985,18 @@ def _arg(t: Optional[torch.Tensor], dtype, shape, dev: int, what: str) -> int:
 
 def _device_of(t: torch.Tensor, what: str) -> int:
     """The device of a call: its first tensor's, which is the current one."""
-    dev = _dev(t, torch.float16, what).get_device()
-    _here(t)
+    _dev(t, torch.float16, what)
     if t.dim() != 2:
         raise ValueError(f"{what} is a matrix")
+    dev = t.get_device()
+    if _current_device is None or dev != _current_device():
+        _here(t)
     return dev
+
+
+def _stream_of(stream, dev: int) -> int:
+    """_stream, of the current device `dev`, which has a tensor."""
+    return _stream(stream) if stream is not None or _current_raw_stream is None else _current_raw_stream(dev)
 
 
 def _lora_h(h: Optional[torch.Tensor], T: int) -> int:
@@ -1024,11 +1029,12 @@ def lora_multitenant(x: torch.Tensor, adapters: LoraTable, tenant_of_token, y0: 
     if workspace is None:
         workspace = new_workspace(lora_workspace_bytes(T, 1, adapters.max_rank), x.device)
     h_ld = _lora_h(h, T)
-    _here(h, workspace, adapters.scale)
+    if h is not None or workspace.get_device() != dev or adapters.device != dev:
+        _here(h, workspace, adapters.scale)
     tok, keep = _tok_pointer(tenant_of_token, T)
     _check(lib().bd_lora_multitenant(x.data_ptr(), adapters.a_ptrs, adapters.b_ptrs, adapters.rank_arr, adapters.scale.data_ptr(), tok,
                                      _arg(y0, torch.float16, (T, out), dev, "y0"), _arg(y, torch.float16, (T, out), dev, "y"), _ptr(h), h_ld,
-                                     T, out, inn, adapters.n_tenants, workspace.data_ptr(), workspace.numel(), _stream(stream)),
+                                     T, out, inn, adapters.n_tenants, workspace.data_ptr(), workspace.numel(), _stream_of(stream, dev)),
            "bd_lora_multitenant")
     return y
 
@@ -1058,11 +1064,12 @@ def lora_multitenant_group(x: torch.Tensor, group: LoraGroup, tenant_of_token, y
         h_ptrs, h_ld = array(*[_ptr(h) or None for h in hs]), widths.pop()
     if workspace is None:
         workspace = new_workspace(lora_workspace_bytes(T, group.n, group.max_rank), x.device)
-    _here(workspace, *group.scales)
+    if workspace.get_device() != dev or group.device != dev:
+        _here(workspace, *group.scales)
     tok, keep = _tok_pointer(tenant_of_token, T)
     _check(lib().bd_lora_multitenant_group(group.n, x.data_ptr(), group.a_ptrs, group.b_ptrs, group.rank_arr, group.scale, tok, y0_ptrs,
                                            y_ptrs, h_ptrs, h_ld, T, group.out_arr, inn, group.n_tenants, workspace.data_ptr(),
-                                           workspace.numel(), _stream(stream)),
+                                           workspace.numel(), _stream_of(stream, dev)),
            "bd_lora_multitenant_group")
     return list(ys)
 
@@ -1107,12 +1114,13 @@ def lora_multitenant_backward(dy: torch.Tensor, x: Optional[torch.Tensor], h: Op
     h_ld = _lora_h(h, T)
     if workspace is None:
         workspace = new_workspace(lora_backward_workspace_bytes(T, out, inn, adapters.n_tenants, adapters.max_rank), dy.device)
-    _here(h, workspace, adapters.scale)
+    if h is not None or workspace.get_device() != dev or adapters.device != dev:
+        _here(h, workspace, adapters.scale)
     tok, keep = _tok_pointer(tenant_of_token, T)
     _check(lib().bd_lora_multitenant_backward(dy.data_ptr(), x_ptr, _ptr(h), h_ld, adapters.a_ptrs, adapters.b_ptrs, adapters.rank_arr,
                                               adapters.scale.data_ptr(), tok, dx0_ptr, dx_ptr, grads.da_ptrs if grads else None,
                                               grads.db_ptrs if grads else None, int(accumulate), T, out, inn, adapters.n_tenants,
-                                              workspace.data_ptr(), workspace.numel(), _stream(stream)), "bd_lora_multitenant_backward")
+                                              workspace.data_ptr(), workspace.numel(), _stream_of(stream, dev)), "bd_lora_multitenant_backward")
     return dx
 
 
