@@ -5,6 +5,7 @@ kernels.  There is no CPU fallback: if the library is missing, loading raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import List, Optional, Sequence
@@ -994,6 +995,16 @@ def _device_of(t: torch.Tensor, what: str) -> int:
     return dev
 
 
+@contextlib.contextmanager
+def _memory_of(stream, dev: int):
+    """Where memory that a call allocates belongs: to the call's stream, so that the allocator hands it on when that stream is done with it."""
+    if stream is None:
+        yield
+        return
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=dev)):
+        yield
+
+
 def _stream_of(stream, dev: int) -> int:
     """_stream, of the current device `dev`, which has a tensor."""
     return _stream(stream) if stream is not None or _current_raw_stream is None else _current_raw_stream(dev)
@@ -1024,10 +1035,10 @@ def lora_multitenant(x: torch.Tensor, adapters: LoraTable, tenant_of_token, y0: 
         out = adapters.shape[0]
     if out is None or (adapters.shape is not None and adapters.shape[1] != inn):
         raise ValueError("x, y and the adapters disagree in shape")
-    if y is None:
-        y = torch.empty((T, out), dtype=torch.float16, device=x.device)
-    if workspace is None:
-        workspace = new_workspace(lora_workspace_bytes(T, 1, adapters.max_rank), x.device)
+    if y is None or workspace is None:
+        with _memory_of(stream, dev):
+            y = y if y is not None else torch.empty((T, out), dtype=torch.float16, device=x.device)
+            workspace = workspace if workspace is not None else new_workspace(lora_workspace_bytes(T, 1, adapters.max_rank), x.device)
     h_ld = _lora_h(h, T)
     if h is not None or workspace.get_device() != dev or adapters.device != dev:
         _here(h, workspace, adapters.scale)
@@ -1047,8 +1058,10 @@ def lora_multitenant_group(x: torch.Tensor, group: LoraGroup, tenant_of_token, y
     T, inn = x.shape
     if group.inn is not None and group.inn != inn:
         raise ValueError("x and the adapters disagree on `in`")
-    if ys is None:
-        ys = [torch.empty((T, o), dtype=torch.float16, device=x.device) for o in group.outs]
+    if ys is None or workspace is None:
+        with _memory_of(stream, dev):
+            ys = ys if ys is not None else [torch.empty((T, o), dtype=torch.float16, device=x.device) for o in group.outs]
+            workspace = workspace if workspace is not None else new_workspace(lora_workspace_bytes(T, group.n, group.max_rank), x.device)
     y0s = list(y0s) if y0s is not None else [None] * group.n
     if len(ys) != group.n or len(y0s) != group.n or (hs is not None and len(hs) != group.n):
         raise ValueError("one y (y0, h) per matrix")
@@ -1062,8 +1075,6 @@ def lora_multitenant_group(x: torch.Tensor, group: LoraGroup, tenant_of_token, y
             raise ValueError("h of one width")
         _here(*hs)
         h_ptrs, h_ld = array(*[_ptr(h) or None for h in hs]), widths.pop()
-    if workspace is None:
-        workspace = new_workspace(lora_workspace_bytes(T, group.n, group.max_rank), x.device)
     if workspace.get_device() != dev or group.device != dev:
         _here(workspace, *group.scales)
     tok, keep = _tok_pointer(tenant_of_token, T)
@@ -1105,15 +1116,17 @@ def lora_multitenant_backward(dy: torch.Tensor, x: Optional[torch.Tensor], h: Op
     inn = adapters.shape[1]
     if adapters.shape[0] != out or (grads is not None and grads.table is not adapters):
         raise ValueError("dy, the adapters and the gradients belong together")
-    if want_dx and dx is None:
-        dx = torch.empty((T, inn), dtype=torch.float16, device=dy.device)
+    if (want_dx and dx is None) or workspace is None:
+        with _memory_of(stream, dev):
+            if want_dx and dx is None:
+                dx = torch.empty((T, inn), dtype=torch.float16, device=dy.device)
+            if workspace is None:
+                workspace = new_workspace(lora_backward_workspace_bytes(T, out, inn, adapters.n_tenants, adapters.max_rank), dy.device)
     if not want_dx:
         dx = dx0 = None
     f16, shape = torch.float16, (T, inn)
     x_ptr, dx0_ptr, dx_ptr = _arg(x, f16, shape, dev, "x"), _arg(dx0, f16, shape, dev, "dx0"), _arg(dx, f16, shape, dev, "dx")
     h_ld = _lora_h(h, T)
-    if workspace is None:
-        workspace = new_workspace(lora_backward_workspace_bytes(T, out, inn, adapters.n_tenants, adapters.max_rank), dy.device)
     if h is not None or workspace.get_device() != dev or adapters.device != dev:
         _here(h, workspace, adapters.scale)
     tok, keep = _tok_pointer(tenant_of_token, T)
@@ -1189,7 +1202,8 @@ def adamw_values(codes: torch.Tensor, second: bool, values: Optional[torch.Tenso
     sign), as float16, which holds the values exactly."""
     _dev(codes, torch.uint8, "codes")
     if values is None:
-        values = torch.empty(codes.shape, dtype=torch.float16, device=codes.device)
+        with _memory_of(stream, codes.get_device()):
+            values = torch.empty(codes.shape, dtype=torch.float16, device=codes.device)
     if _dev(values, torch.float16, "values").numel() != codes.numel():
         raise ValueError("one value per code")
     _here(codes, values)

@@ -168,3 +168,23 @@ def test_weights_that_are_not_finite_stay_in_their_row(bd, T, rank):
     dx, dz = (bd.lora_multitenant_backward(y0, None, None, t, tok, None, dx0=x) for t in (table, with_a))
     others = [f for f in range(inn) if f != column]
     assert torch.equal(dx[:, others], dz[:, others]) and not torch.isfinite(dz[:, column]).any()
+
+
+def test_memory_of_a_call_belongs_to_its_stream(bd, monkeypatch):
+    """Without a workspace a call allocates one: of its own stream, not of the current one, which may hand the memory on too early."""
+    a, b, scale, x, y0 = ref64.make([16, 20], 136, 64, 40, seed=3)
+    table = bd.LoraTable(a, b, scale)
+    tok = [t % 2 for t in range(40)]
+    want = bd.lora_multitenant(x, table, tok, y0=y0)
+    want_dx = bd.lora_multitenant_backward(y0, None, None, table, tok, None, dx0=x)
+    torch.cuda.synchronize()
+    seen, make = [], bd.new_workspace
+    monkeypatch.setattr(bd, "new_workspace", lambda n, device: (seen.append(torch.cuda.current_stream().cuda_stream), make(n, device))[1])
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        y = bd.lora_multitenant(x, table, tok, y0=y0, stream=stream)
+        ys = bd.lora_multitenant_group(x, bd.LoraGroup([table], [136]), tok, y0s=[y0], stream=stream)
+        dx = bd.lora_multitenant_backward(y0, None, None, table, tok, None, dx0=x, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(ys[0], want) and torch.equal(dx, want_dx)
+    assert seen == [side.cuda_stream] * 6
