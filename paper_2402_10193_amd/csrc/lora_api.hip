@@ -230,8 +230,8 @@ bd_status forward(int32_t n_mats, const uint16_t* x, const uint16_t* const* a_by
         if (out[m] > 0 && !y[m]) return BD_ERR_NULL;
         if (misaligned(y[m], 16) || (y0 && misaligned(y0[m], 16)) || misaligned(scale[m], 4) || (h && misaligned(h[m], 4))) return BD_ERR_ALIGN;
         if (max_rank > 0 && out[m] > 0 && !scale[m]) return BD_ERR_NULL;
+        if (h && h[m] && (h_ld < 0 || h_ld < max_rank)) return BD_ERR_SHAPE;
         const size_t hbytes = h && h[m] ? (size_t)T * h_ld * 4 : 0;
-        if (hbytes && h_ld < max_rank) return BD_ERR_SHAPE;
         if (overlaps(y[m], ybytes, x, xbytes) || (hbytes && (overlaps(h[m], hbytes, x, xbytes) || overlaps(h[m], hbytes, y[m], ybytes)))) return BD_ERR_ALIAS;
         for (int o = 0; o < n_mats; ++o) {
             const size_t obytes = (size_t)T * out[o] * 2;
