@@ -109,7 +109,7 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 
 // g and h as operands of the gradients' sums over tokens, in chunks of 32 tokens of a job
 struct LoraPrepJob {
-    int32_t first, count, rank, chunk_begin;
+    int32_t first, count, rank, chunk_begin, sides;   // sides: bit 0 where g is wanted, bit 1 where h is
 };
 struct LoraPrepArgs {
     float* g;                           // [splits][rows][ld] by sorted position; part 0 receives the sum

@@ -460,12 +460,13 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
     int64_t groups = 0;
     for (const Job& j : batch.jobs) groups += (int64_t)(j.count + columns - 1) / columns * bd::lora_shrink_groups(rank_by[j.tenant], columns);
     int splits = sum_splits(groups, out, T, T, ld, few, any_da || any_db ? 0 : rows_again(batch, in, columns));
-    auto weights_of = [&](const uint16_t* const* by, bool all) {
-        return [=](int, int32_t tenant, const uint16_t** w, int* rank) {
-            *rank = rank_by[tenant];
-            *w = by && *rank > 0 ? by[tenant] : nullptr;
-            return all || *rank > 0;
-        };
+    // A tenant's g (and B) where dx or its own dA is wanted.  (The sum is cut as if all were: what else is wanted does not change its bits.)
+    auto wants_da = [&](int32_t tenant) { return any_da && da_by && da_by[tenant]; };
+    auto wants_db = [&](int32_t tenant) { return any_db && db_by && db_by[tenant]; };
+    auto wants_g = [&](int32_t tenant) { return want_dx || wants_da(tenant); };
+    auto weights_of = [&](const uint16_t* const* by, int32_t tenant, const uint16_t** w, int* rank) {
+        *rank = rank_by[tenant];
+        *w = by && *rank > 0 ? by[tenant] : nullptr;
     };
     if (work && (want_dx || any_da)) {
         auto s = std::make_unique<bd::LoraShrinkArgs>();
@@ -477,8 +478,14 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         s->ld = (int32_t)ld;
         s->splits = splits;
         s->split_stride = T * ld;
-        if (for_records(*s, batch, T, 1, columns, weights_of(b_by, false), [&](int rank, bool odd) { return bd::launch_lora_shrink(*s, columns, true, rank, odd, st); }) != hipSuccess)
-            return BD_ERR_DEVICE;
+        const hipError_t e = for_records(
+            *s, batch, T, 1, columns,
+            [&](int, int32_t tenant, const uint16_t** w, int* rank) {
+                weights_of(b_by, tenant, w, rank);
+                return *rank > 0 && wants_g(tenant);
+            },
+            [&](int rank, bool odd) { return bd::launch_lora_shrink(*s, columns, true, rank, odd, st); });
+        if (e != hipSuccess) return BD_ERR_DEVICE;
     }
     // ---- g (parts added up) and h as operands of the gradients ----
     const int64_t chunks_most = most_chunks(T, n_tenants);
@@ -514,7 +521,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         prep->h_ld = h_ld;
         prep->side_first = any_da ? 0 : 1;
         args->accumulate = accumulate ? 1 : 0;
-        std::vector<Job> wanted;   // (all with a rank: the sum of g's parts is the expand's input too)
+        std::vector<Job> wanted;   // (all with a rank: the sum of g's parts is the expand's input too, and what else is wanted cuts no sum otherwise)
         for (const Job& j : batch.jobs)
             if (rank_by[j.tenant] > 0) wanted.push_back(j);
         int32_t chunk = 0;
@@ -525,7 +532,7 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
             for (int i = 0; i < n; ++i) {
                 const Job& j = wanted[first + (size_t)i];
                 const int rank = rank_by[j.tenant];
-                prep->job[i] = bd::LoraPrepJob{j.first, j.count, rank, chunk};
+                prep->job[i] = bd::LoraPrepJob{j.first, j.count, rank, chunk, (any_da && wants_g(j.tenant) ? 1 : 0) | (wants_db(j.tenant) ? 2 : 0)};
                 args->job[i] = bd::LoraGradJob{{da_by && in > 0 ? da_by[j.tenant] : nullptr, db_by && out > 0 ? db_by[j.tenant] : nullptr},
                                                0, j.tenant, j.count, j.first, rank, chunk, 1, 0};
                 chunk += (j.count + 31) / 32;
@@ -577,8 +584,14 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
         x2->ld = (int32_t)ld;
         x2->splits = splits;
         x2->split_stride = T * ld;
-        if (for_records(*x2, batch, T, 1, columns, weights_of(a_by, dx0 != dx), [&](int rank, bool odd) { return bd::launch_lora_expand(*x2, columns, true, rank, in, in, odd, st); }) != hipSuccess)
-            return BD_ERR_DEVICE;
+        const hipError_t e = for_records(
+            *x2, batch, T, 1, columns,
+            [&](int, int32_t tenant, const uint16_t** w, int* rank) {
+                weights_of(a_by, tenant, w, rank);
+                return *rank > 0 || dx0 != dx;
+            },
+            [&](int rank, bool odd) { return bd::launch_lora_expand(*x2, columns, true, rank, in, in, odd, st); });
+        if (e != hipSuccess) return BD_ERR_DEVICE;
     }
     if (!accumulate) {   // gradients of adapters that no token used
         auto zero = std::make_unique<bd::LoraReduceArgs>();

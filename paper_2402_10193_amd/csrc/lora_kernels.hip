@@ -925,6 +925,7 @@ __global__ __launch_bounds__(kPrepThreads) void lora_prep_kernel(const LoraPrepA
     const int j = __builtin_amdgcn_readfirstlane(__popcll(__ballot(record < a.n_jobs && a.job[min(record, a.n_jobs - 1)].chunk_begin <= (int)blockIdx.x + a.chunk_first)) - 1);
     const LoraPrepJob& job = a.job[j];
     const bool of_h = blockIdx.y + a.side_first == 1;
+    if (!(job.sides >> (int)of_h & 1)) return;   // (nobody has written this tenant's g, or nobody reads what h would become)
     const int chunk = blockIdx.x + a.chunk_first, t0 = (chunk - job.chunk_begin) * 32, rank_all = job.rank, tiles = (rank_all + 15) / 16;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = lane & 15, q = lane >> 4;
     constexpr int kMine = kLoraMaxRank / 16 / (kPrepThreads / kWave);   // rank tiles of a wavefront

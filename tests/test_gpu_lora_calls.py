@@ -1,0 +1,54 @@
+"""Calls of the low-rank adapters that lie between the ordinary ones: gradients of some tenants only, inputs that no wanted result needs."""
+import pytest
+import torch
+
+import lora_ref as ref64
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def bd():
+    from paper_2402_10193_amd import binding
+    return binding
+
+
+def _gradients(ranks, out, inn, da=None, db=None):
+    """Gradients full of 7 for the tenants in `da` and `db` (all that have an adapter where not given)."""
+    some = lambda which, e: ranks[e] > 0 and (which is None or e in which)
+    return ([torch.full((r, inn), 7.0, device=DEV) if some(da, e) else None for e, r in enumerate(ranks)],
+            [torch.full((out, r), 7.0, device=DEV) if some(db, e) else None for e, r in enumerate(ranks)])
+
+
+@pytest.mark.parametrize("T", [4, 40, 600, 5000])
+@pytest.mark.parametrize("mixed", [True, False])
+def test_gradients_of_some_tenants(bd, T, mixed):
+    """Frozen tenants among trained ones: no A of anyone and no B of a tenant whose dA is not wanted.  The gradients are right, and the bits
+    those of the same call with every weight given."""
+    print(f"gradients of some tenants T={T} mixed={mixed}", flush=True)
+    out, inn, ranks = 264, 128, [8, 17, 0, 16]
+    a, b, scale, x, dy = ref64.make(ranks, out, inn, T, seed=T)
+    tok = [(5 * t + t // 7) % 4 for t in range(T)]
+    tok = tok if mixed else sorted(tok)
+    h = torch.randn((T, 17), generator=torch.Generator().manual_seed(1)).to(DEV)
+    table = bd.LoraTable(a, b, scale)
+    _, _, want = ref64.backward(dy, x, h, a, b, scale, tok, None)
+    for want_a, want_b in (([0], [1]), ([3], []), ([0, 1], [3]), ([], [0])):
+        part = bd.LoraTable(a, b, scale)
+        for e in range(4):
+            part.a_ptrs[e] = None
+            if e not in want_a:
+                part.b_ptrs[e] = None
+        results = []
+        for weights in (part, table):
+            da, db = _gradients(ranks, out, inn, want_a, want_b)
+            bd.lora_multitenant_backward(dy, x if want_a else None, h if want_b else None, weights, tok, bd.LoraGrads(weights, da, db), want_dx=False)
+            results.append((da, db))
+        (da, db), (da2, db2) = results
+        for e in want_a:
+            ref64.check(da[e], want[e][0], want[e][1], f"dA of tenant {e}")
+            assert torch.equal(da[e], da2[e])
+        for e in want_b:
+            ref64.check(db[e], want[e][2], want[e][3], f"dB of tenant {e}")
+            assert torch.equal(db[e], db2[e])
