@@ -440,7 +440,7 @@ bd_status bd_linear_multitenant_tiled_group_q8(int32_t n_mats, const uint16_t* x
  *   a_by_tenant, b_by_tenant   HOST arrays of n_tenants DEVICE pointers; NULL allowed for tenants without a token and where
  *                    the rank is 0
  *   rank_by_tenant   HOST [n_tenants], 0 .. BD_LORA_MAX_RANK each (checked for tenants with a token); 0: no adapter, y[t] = y0[t] bit by bit
- *   scale_by_tenant  device array of n_tenants floats
+ *   scale_by_tenant  device array of n_tenants floats; NULL allowed where out = 0 or no token has an adapter
  *   tenant_of_token  HOST [T], any order; tokens are grouped by tenant inside the call
  *   y0_f16, y_f16    [T, out]; y0 may be NULL (zeros) or y itself, but not overlap y otherwise
  *   h                NULL, or device [T, h_ld] floats that receive h[t][0 .. r_e) for the backward pass; h_ld >= the largest rank

@@ -528,7 +528,8 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
     // read element by element
     const int64_t f0 = ((int64_t)blockIdx.y * kLoraExpandWaves + wave) * kLoraFeatures, base = min(f0, max(F - kLoraFeatures, (int64_t)0)), f = base + 8 * m;
     const bool active = f0 < F, vectors = ROWS != kShortRows || F >= kLoraFeatures;
-    const float scale = u.rank == 0 ? -0.0f : TR ? 1.0f : a.scale[u.mat][u.tenant];   // (y0 + 0 * -0 is y0, also where it is -0)
+    // (y0 + 0 * -0 is y0, also where it is -0; a matrix without outputs, whose h alone is asked for, may have no scales)
+    const float scale = u.rank == 0 ? -0.0f : TR || F == 0 ? 1.0f : a.scale[u.mat][u.tenant];
 
     int64_t at[4];   // where the lane's results belong: token 4 g + i
     half8 before[4];
@@ -708,7 +709,8 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     // Features f0 .. f0 + 127; a row's last 128 end with it, and of them only those from f0 on are kept.  A row below 128 is read element
     // by element.
     int64_t f0 = (int64_t)blockIdx.y * kLoraFeatures;
-    const float scale = u.rank == 0 ? -0.0f : TR ? 1.0f : a.scale[u.mat][u.tenant];   // (y0 + 0 * -0 is y0, also where it is -0)
+    // (y0 + 0 * -0 is y0, also where it is -0; a matrix without outputs, whose h alone is asked for, may have no scales)
+    const float scale = u.rank == 0 ? -0.0f : TR || F == 0 ? 1.0f : a.scale[u.mat][u.tenant];
     const bool vectors = ROWS != kShortRows || F >= kLoraFeatures;
     auto begin_of = [&](int64_t first) { return min(first, max(F - kLoraFeatures, (int64_t)0)); };
 

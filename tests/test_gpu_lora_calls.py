@@ -52,3 +52,28 @@ def test_gradients_of_some_tenants(bd, T, mixed):
         for e in want_b:
             ref64.check(db[e], want[e][2], want[e][3], f"dB of tenant {e}")
             assert torch.equal(db[e], db2[e])
+
+
+@pytest.mark.parametrize("T", [2, 20, 600])
+@pytest.mark.parametrize("rank", [5, 16, 40])
+def test_h_alone_needs_no_scales(bd, T, rank):
+    """A matrix without outputs whose h is asked for, alone and beside another one: scales, y and B may be missing."""
+    print(f"h alone T={T} rank={rank}", flush=True)
+    inn, out = 96, 40
+    a, b, scale, x, y0 = ref64.make([rank, 8], out, inn, T, seed=T + rank)
+    tok = [t % 2 for t in range(T)]
+    none = bd.LoraTable(a, [torch.empty((0, t.shape[1]), dtype=torch.float16, device=DEV) for t in b], scale)
+    _, h_of, _ = ref64.forward(x, a, b, scale, tok, y0, out)
+    for both in (False, True):
+        tables = [bd.LoraTable(a, b, scale), none] if both else [none]
+        group = bd.LoraGroup(tables, [out, 0] if both else [0])
+        group.scale[group.n - 1] = None
+        hs = [torch.zeros((T, max(rank, 8)), device=DEV) for _ in tables]
+        ys = bd.lora_multitenant_group(x, group, tok, y0s=[y0, None] if both else [None], hs=hs)
+        for e, (rows, want) in h_of.items():
+            size = x[rows].double().abs() @ a[e].double().abs().t()
+            for h in hs:
+                ref64.check(h[rows, :want.shape[1]], want, (inn / 8 + 16) * ref64.U32 * size + 1e-30, f"h of tenant {e}")
+        if both:
+            want, _, bound = ref64.forward(x, a, b, scale, tok, y0, out)
+            ref64.check(ys[0], want, bound, "y")
