@@ -369,7 +369,7 @@ __global__ __launch_bounds__(kShrinkThreads) void lora_shrink_kernel(const LoraS
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         if constexpr (TR) {
-            const int at = lane + kWave * r, per_row = width / 8;
+            const int at = lane + kWave * r, per_row = max(width / 8, 1);   // (below 8 ranks there are no whole pieces: not used)
             // (a lane without a piece of its own reads and stores one of the last row's once more: no branches)
             const int over = (int)(((unsigned)at * (65536u / (unsigned)per_row + 1)) >> 16);   // at / per_row
             piece_row[r] = pieces ? min(over, 31) : 0;

@@ -77,3 +77,23 @@ def test_h_alone_needs_no_scales(bd, T, rank):
         if both:
             want, _, bound = ref64.forward(x, a, b, scale, tok, y0, out)
             ref64.check(ys[0], want, bound, "y")
+
+
+@pytest.mark.parametrize("T", [60, 900])
+@pytest.mark.parametrize("out", [20, 33, 160])
+@pytest.mark.parametrize("ranks", [[1, 2, 3, 4, 5, 6, 7], [17, 18, 8, 33, 39, 41]])
+def test_gradients_of_ranks_without_whole_pieces(bd, T, out, ranks):
+    """A last block of 16 ranks with fewer than 8 in it, and no other."""
+    print(f"no whole pieces T={T} out={out} ranks={ranks}", flush=True)
+    inn, n = 64, len(ranks)
+    a, b, scale, x, dy = ref64.make(ranks, out, inn, T, seed=T + out)
+    tok = [(3 * t) % n for t in range(T)]
+    h = torch.randn((T, max(ranks)), generator=torch.Generator().manual_seed(2)).to(DEV)
+    table = bd.LoraTable(a, b, scale)
+    da, db = _gradients(ranks, out, inn)
+    dx = bd.lora_multitenant_backward(dy, x, h, table, tok, bd.LoraGrads(table, da, db))
+    want, bound, grads = ref64.backward(dy, x, h, a, b, scale, tok, None)
+    ref64.check(dx, want, bound, "dx")
+    for e, (ga, ga_bound, gb, gb_bound) in grads.items():
+        ref64.check(da[e], ga, ga_bound, f"dA of tenant {e}")
+        ref64.check(db[e], gb, gb_bound, f"dB of tenant {e}")
