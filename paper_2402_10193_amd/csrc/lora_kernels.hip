@@ -1071,7 +1071,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(OD
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int row = mine + 4 * i;
-            *(half8*)&tile[row][8 * n] = 32 * chunk + row < count ? rows[b][i] : half8{};   // (beyond the part's last tile: all zeros)
+            *(half8*)&tile[row][8 * n] = 32 * chunk + row < count ? rows[b][i] : half8{};
         }
         load_rows(b, k + 2);
         load_operand(1 - b, k + 1);
@@ -1079,6 +1079,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(OD
             __syncthreads();
         else
             __builtin_amdgcn_wave_barrier();
+        if (chunk >= chunks) return;   // (of the whole group: rows of zeros times an infinity of the last tile's operand would be NaN)
         const int now = exponent[b];
         if (now >= largest - 64) {
             largest = max(largest, now);
@@ -1109,7 +1110,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(OD
     load_operand(0, 0);
     load_rows(0, 0);
     load_rows(1, 1);
-    for (int k = 0; TW * k < chunks; k += 2) {   // (of the whole workgroup; steps beyond the last bring zeros)
+    for (int k = 0; TW * k < chunks; k += 2) {   // (of the whole workgroup; steps beyond the last bring nothing)
         step(std::integral_constant<int, 0>{}, k);
         step(std::integral_constant<int, 1>{}, k + 1);
     }

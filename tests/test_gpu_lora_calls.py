@@ -97,3 +97,31 @@ def test_gradients_of_ranks_without_whole_pieces(bd, T, out, ranks):
     for e, (ga, ga_bound, gb, gb_bound) in grads.items():
         ref64.check(da[e], ga, ga_bound, f"dA of tenant {e}")
         ref64.check(db[e], gb, gb_bound, f"dB of tenant {e}")
+
+
+def _same_as_formula(got, want, what):
+    """Infinities where the formula in 64 bits has them, with their signs, NaN where it has them, and no other."""
+    got = got.double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaN at {int(torch.isnan(got).sum())} places, {int(torch.isnan(want).sum())} by the formula"
+    for bad in (float("inf"), -float("inf")):
+        assert torch.equal(got == bad, want == bad), f"{what}: {bad} at {int((got == bad).sum())} places, {int((want == bad).sum())} by the formula"
+
+
+@pytest.mark.parametrize("T,at", [(5, 3), (32, 0), (33, 32), (96, 70), (128, 127), (129, 128), (700, 699), (4200, 4199)])
+@pytest.mark.parametrize("rank", [8, 24, 64])
+def test_infinite_operands_of_the_gradients(bd, T, at, rank):
+    """An infinity of h makes its column of dB infinite, one of g its row of dA: with the formula's sign, however many tiles of tokens there are."""
+    print(f"infinite operands T={T} at={at} rank={rank}", flush=True)
+    out, inn = 136, 160
+    a, b, scale, x, dy = ref64.make([rank], out, inn, T, seed=T)
+    h = torch.randn((T, rank), generator=torch.Generator().manual_seed(3)).to(DEV)
+    h[at, 2], h[at, rank - 1] = float("inf"), -float("inf")
+    table = bd.LoraTable(a, b, scale)
+    _, db = _gradients([rank], out, inn)
+    bd.lora_multitenant_backward(dy, None, h, table, [0] * T, bd.LoraGrads(table, [None], db), want_dx=False)
+    _same_as_formula(db[0], float(scale[0]) * (dy.double().t() @ h.double()), "dB")
+    dy[at, 7] = float("inf")                             # g of this token, all ranks, by the sign of B
+    da, _ = _gradients([rank], out, inn)
+    bd.lora_multitenant_backward(dy, x, None, table, [0] * T, bd.LoraGrads(table, da, [None]), want_dx=False)
+    g = float(scale[0]) * (dy.double() @ b[0].double())
+    _same_as_formula(da[0], g.t() @ x.double(), "dA")
