@@ -435,7 +435,9 @@ bd_status bd_linear_multitenant_tiled_group_q8(int32_t n_mats, const uint16_t* x
  * These calls add what the adapters of ALL tokens of a batch give to what the shared projection gave, whichever of the linears
  * above that was (an fp16 or 8-bit base, row-major or tiled, with or without 1-bit deltas):
  *     h[t] = A_e x[t]                                  e = tenant_of_token[t]
- *     y[t] = fp16( f32(y0[t]) + s_e * (B_e h[t]) )     one rounding; sums in binary32, h to 22 bits or more
+ *     y[t] = fp16( f32(y0[t]) + s_e * (B_e h[t]) )     one rounding; sums in binary32
+ * A value of h (of g below) that goes into a matrix-core product keeps 22 bits, or of a value that is far smaller what lies above 2^-39
+ * of the largest of its GROUP (and above 2^-125): a token's ranks for y and dx, 32 tokens of one rank for dB and dA.
  *   x_f16            [T, in]
  *   a_by_tenant, b_by_tenant   HOST arrays of n_tenants DEVICE pointers; NULL allowed for tenants without a token and where
  *                    the rank is 0
@@ -468,7 +470,7 @@ bd_status bd_lora_multitenant_group(int32_t n_mats, const uint16_t* x_f16, const
                                     int32_t n_tenants, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The gradients of bd_lora_multitenant, for training the adapters of several tenants at once:
- *     g[t]  = s_e B_e^T dy[t]                       (binary32, to 22 bits or more where it is multiplied on)
+ *     g[t]  = s_e B_e^T dy[t]                       binary32
  *     dx[t] = fp16( f32(dx0[t]) + A_e^T g[t] )      dx0: the gradient through the shared projection, NULL (zeros) or dx itself
  *     dA_e  = sum over e's tokens of g[t] x[t]^T    binary32 [r_e, in]
  *     dB_e  = s_e * sum of dy[t] h[t]^T             binary32 [out, r_e]

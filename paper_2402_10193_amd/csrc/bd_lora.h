@@ -116,7 +116,7 @@ struct LoraPrepArgs {
     const float* h;                     // [T, h_ld] by token
     const int32_t* order;
     half8* operand[2];                  // of g, of h: [chunk][ld / 16][hi, lo][64 lanes]
-    int32_t* exponent[2];               // [chunk]
+    uint8_t* exponent[2];               // [chunk][ld]: 127 + e, by rank
     int64_t split_stride;
     int32_t ld, splits, h_ld, n_jobs, chunk_first, side_first;   // side_first = 1: only h
     LoraPrepJob job[kLoraRecords];
@@ -134,7 +134,7 @@ struct LoraGradJob {
 struct LoraGradSide {
     const uint16_t* d;                  // [T, F]
     const half8* operand;
-    const int32_t* exponent;
+    const uint8_t* exponent;
     const float* scale;                 // dB: device, by tenant; dA: nullptr (g has it)
     float* partial;                     // the sums of jobs whose tokens are in several parts: [part][rank * F]
     int64_t F;

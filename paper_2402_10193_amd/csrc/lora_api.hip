@@ -175,10 +175,10 @@ size_t order_bytes(int64_t T) { return (size_t)round_up(T * 4, 256); }
 size_t h_bytes(int64_t T, int32_t n_mats, int32_t max_rank) {
     return (size_t)round_up((int64_t)max_splits(T) * n_mats * T * round_up(max_rank, 16) * 4, 256);
 }
-// operands of the gradients: 32 tokens of a job by 16 ranks as hi and lo, for g and for h, and their exponents
+// operands of the gradients: 32 tokens of a job by 16 ranks as hi and lo, for g and for h, and an exponent for every rank of the 32
 int64_t most_chunks(int64_t T, int32_t n_tenants) { return T / 32 + std::min<int64_t>(T, n_tenants); }
 size_t operand_bytes(int64_t chunks, int32_t max_rank) { return (size_t)(chunks * (round_up(max_rank, 16) / 16) * 2 * 64 * 16); }
-size_t exponent_bytes(int64_t chunks) { return (size_t)round_up(chunks * 4, 256); }
+size_t exponent_bytes(int64_t chunks, int32_t max_rank) { return (size_t)round_up(chunks * round_up(max_rank, 16), 256); }
 int64_t most_parts(int64_t T) { return std::min<int64_t>(kGradParts, T / 32); }
 size_t grad_part_bytes(int64_t T, int64_t out, int64_t in, int32_t max_rank) {
     return (size_t)round_up(most_parts(T) * round_up(max_rank, 16) * (in + out) * 4, 256);
@@ -490,12 +490,12 @@ bd_status backward(const uint16_t* dy, const uint16_t* x, const float* h, int32_
     // ---- g (parts added up) and h as operands of the gradients ----
     const int64_t chunks_most = most_chunks(T, n_tenants);
     bd::half8* operand[2] = {nullptr, nullptr};
-    int32_t* exponent[2] = {nullptr, nullptr};
+    uint8_t* exponent[2] = {nullptr, nullptr};
     float* partial = nullptr;
     if (work) {
         char* p = (char*)g + h_bytes(T, 1, max_rank);
         for (int side = 0; side < 2; ++side, p += operand_bytes(chunks_most, max_rank)) operand[side] = (bd::half8*)p;
-        for (int side = 0; side < 2; ++side, p += exponent_bytes(chunks_most)) exponent[side] = (int32_t*)p;
+        for (int side = 0; side < 2; ++side, p += exponent_bytes(chunks_most, max_rank)) exponent[side] = (uint8_t*)p;
         partial = (float*)p;
     }
     if (work && (any_da || any_db)) {
@@ -633,7 +633,7 @@ size_t bd_lora_workspace_bytes(int64_t T, int32_t n_mats, int32_t max_rank) {
 size_t bd_lora_backward_workspace_bytes(int64_t T, int64_t out, int64_t in, int32_t n_tenants, int32_t max_rank) {
     if (T < 1 || !sizes_ok(T, out, in, n_tenants) || n_tenants < 1 || max_rank < 1 || max_rank > bd::kLoraMaxRank) return 0;
     const int64_t chunks = most_chunks(T, n_tenants);
-    return order_bytes(T) + h_bytes(T, 1, max_rank) + 2 * (operand_bytes(chunks, max_rank) + exponent_bytes(chunks)) + grad_part_bytes(T, out, in, max_rank);
+    return order_bytes(T) + h_bytes(T, 1, max_rank) + 2 * (operand_bytes(chunks, max_rank) + exponent_bytes(chunks, max_rank)) + grad_part_bytes(T, out, in, max_rank);
 }
 
 // (what the standard library throws here is a lack of host memory)

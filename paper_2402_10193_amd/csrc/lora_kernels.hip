@@ -7,9 +7,9 @@
 // The ranks are a few to a few dozen, so that every product here is bound by the activations it streams (x, dy, y0, y) or, in
 // a decode step, by latency; the matrix cores have room to spare.  That room buys precision: h and g are held in binary32 and
 // enter the matrix cores as two binary16 numbers each, hi = fp16(v 2^-e) and lo = fp16(v 2^-e - hi), some 22 bits together.  e
-// brings the largest of a token's values (grad: of a wavefront's values) to 2^14 .. 2^15, so that neither part leaves the
-// range of binary16 whatever the scale of the activations or of the loss.  x, dy, A and B are binary16 as they are, the sums
-// binary32.
+// brings the largest of a token's values (grad: of a rank's values in 32 tokens) to 2^14 .. 2^15, so that neither part leaves the
+// range of binary16 whatever the scale of the activations or of the loss: a value keeps 22 bits, or what lies above 2^-39 of the
+// largest of those it is added up with.  x, dy, A and B are binary16 as they are, the sums binary32.
 //
 // v_mfma_f32_16x16x32_f16: lane l = (r, g) = (l % 16, l / 16) supplies row r, elements 8 g .. 8 g + 7 of either operand; result
 // register i of lane (n, q) is element (4 q + i, n).
@@ -918,9 +918,9 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
 
 constexpr int kPrepThreads = 256;
 
-// The second operand of the gradients, once for all their workgroups: 32 tokens' g (or h) as hi and lo in matrix-core order, one
-// exponent for the 32.  Lane (n, q) holds rank n of its 16, tokens 8 q .. 8 q + 7, in 16 bytes.  Where g came in parts their sum
-// takes the first part's place.  Once for 8192 tokens of rank 64: 6 us; in the workgroups of the sums, each for itself: 3 us less for 32
+// The second operand of the gradients, once for all their workgroups: 32 tokens' g (or h) as hi and lo in matrix-core order, with an
+// exponent for each rank (ranks share no sum: the weakest is held as well as the strongest).  Lane (n, q) holds rank n of its 16,
+// tokens 8 q .. 8 q + 7, in 16 bytes.  Where g came in parts their sum takes the first part's place.  Once for 8192 tokens of rank 64: 6 us; in the workgroups of the sums, each for itself: 3 us less for 32
 // tokens per tenant, up to twice the sums' time for 64 tenants or 512 tokens.
 __global__ __launch_bounds__(kPrepThreads) void lora_prep_kernel(const LoraPrepArgs a) {
     const int record = threadIdx.x & (kWave - 1);
@@ -946,14 +946,14 @@ __global__ __launch_bounds__(kPrepThreads) void lora_prep_kernel(const LoraPrepA
         for (int i = 0; i < 8; ++i) at[i] = (int64_t)p[i] * (of_h ? a.h_ld : a.ld);
     }
     const int splits = of_h ? 1 : a.splits;
-    float v[kMine][8];
-    float top = 0.0f;
+    half8* const out = a.operand[of_h] + (int64_t)chunk * (a.ld / 16) * 2 * kWave;
 #pragma unroll
     for (int k = 0; k < kMine; ++k) {
         const int rt = wave + k * (kPrepThreads / kWave), rank = 16 * rt + n, column = min(rank, rank_all - 1);
         if (rt >= tiles) continue;
+        float v[8], top = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[k][i] = src[at[i] + column];
+        for (int i = 0; i < 8; ++i) v[i] = src[at[i] + column];
         for (int s = 1; s < splits; s += 4) {   // the loads of four parts at a time
             float w[4][8];
 #pragma unroll
@@ -963,36 +963,25 @@ __global__ __launch_bounds__(kPrepThreads) void lora_prep_kernel(const LoraPrepA
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[k][i] += s + c < splits ? w[c][i] : 0.0f;
+                for (int i = 0; i < 8; ++i) v[i] += s + c < splits ? w[c][i] : 0.0f;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const bool real = t0 + 8 * q + i < job.count && rank < rank_all;
-            if (splits > 1 && real) a.g[at[i] + column] = v[k][i];
-            v[k][i] = real ? v[k][i] : 0.0f;
-            top = fmaxf(top, finite_abs(v[k][i]));
+            if (splits > 1 && real) a.g[at[i] + column] = v[i];
+            v[i] = real ? v[i] : 0.0f;
+            top = fmaxf(top, finite_abs(v[i]));
         }
-    }
-#pragma unroll
-    for (int d = 32; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
-    __shared__ float tops[kPrepThreads / kWave];
-    if (lane == 0) tops[wave] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kPrepThreads / kWave; ++w) top = fmaxf(top, tops[w]);
-    const int e = group_exponent(top);
-    if (threadIdx.x == 0) a.exponent[of_h][chunk] = e;
-    const float down = power_of_two(-e);
-    half8* const out = a.operand[of_h] + (int64_t)chunk * (a.ld / 16) * 2 * kWave;
-#pragma unroll
-    for (int k = 0; k < kMine; ++k) {
-        const int rt = wave + k * (kPrepThreads / kWave);
-        if (rt >= tiles) continue;
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));   // of the rank's 32 tokens
+        const int e = group_exponent(top);
+        if (q == 0) a.exponent[of_h][(int64_t)chunk * a.ld + rank] = (uint8_t)(127 + e);
+        const float down = power_of_two(-e);
         half8 hi, lo;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             _Float16 h, l;
-            split_half(v[k][i], down, &h, &l);
+            split_half(v[i], down, &h, &l);
             hi[i] = h;
             lo[i] = l;
         }
@@ -1007,8 +996,8 @@ constexpr int kGradPitch = 128 + 16;   // halves: 4 rows apart on banks of their
 // dA or dB of one job: 128 features by 16 RW ranks, summed over one part of the job's tokens.  RW wavefronts with 16 ranks each share a
 // tile of 32 tokens' x (dy); 4 / RW such groups take the tiles in turn and meet in LDS at the end.  The tokens are the sum's index, so
 // both operands want 8 tokens of one feature (rank) in a lane: the second comes prepared, the tile goes through LDS as it is (256 bytes
-// of a row from 16 lanes) and is read transposed.  The sums are kept in units of the present tile's exponent; tiles whose largest value
-// is 2^-64 of the largest so far are below what binary32 would keep of them.
+// of a row from 16 lanes) and is read transposed.  A tile's products are added up in the matrix cores in units of their rank's 2^e
+// and then go into the sum, whatever the sizes of the tiles before.
 // Loads are never under a condition (past the end they repeat the last tile's), or the wait for them would be for all.
 // Bound by the streams of x and dy: 4096 tokens of 8 tenants, 4096 -> 4096, rank 16 (67 MB) 22 us, 3.0 TB/s; 8192 of 2, 4096 -> 11008, rank 64
 // (247 MB) 66 us, 3.7 TB/s.
@@ -1043,7 +1032,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(OD
     const uint16_t* const d = side.d + (ODD && fl >= F ? F - 1 : fl);
     const int64_t last = ODD ? max(F - 1 - fl, (int64_t)0) : 7;
     half8 rows[2][N], op[2][2];
-    int exponent[2];
+    uint8_t exponent[2];   // 127 + e of the lane's rank
     const int mine = rank_wave * 4 * N + q;   // the lane's rows of a tile: mine, mine + 4, ...
     auto chunk_at = [&](int k) { return min(TW * k + group, chunks - 1); };
     auto load_rows = [&](int buffer, int k) {
@@ -1054,16 +1043,14 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(OD
             rows[buffer][i] = !ODD || F >= kLoraFeatures ? load8(p) : load8_each(p, last);
         }
     };
-    typedef const __attribute__((address_space(4))) int32_t* scalar_ints;
     auto load_operand = [&](int buffer, int k) {   // (a wavefront without ranks takes the last's)
         const int chunk = job.chunk_begin + c0 + chunk_at(k), rt = min(rt0 + rank_wave, (rank_all - 1) / 16);
-        exponent[buffer] = ((scalar_ints)side.exponent)[__builtin_amdgcn_readfirstlane(chunk)];
+        exponent[buffer] = side.exponent[(int64_t)chunk * a.ld + 16 * rt + n];
         const half8* const p = side.operand + ((int64_t)chunk * (a.ld / 16) + rt) * 2 * kWave + lane;
         op[buffer][0] = p[0];
         op[buffer][1] = p[kWave];
     };
     float4v acc[8] = {};
-    int e = -200, largest = -200;   // none yet
     auto step = [&](auto which_buffer, int k) {
         constexpr int b = decltype(which_buffer)::value;
         Tile& tile = ((Tile*)lds)[(RW > 1 ? b : 0) * TW + group];
@@ -1080,20 +1067,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(OD
         else
             __builtin_amdgcn_wave_barrier();
         if (chunk >= chunks) return;   // (of the whole group: rows of zeros times an infinity of the last tile's operand would be NaN)
-        const int now = exponent[b];
-        if (now >= largest - 64) {
-            largest = max(largest, now);
-            if (now != e && e > -200) {
-                const float f = power_of_two(max(e - now, -126));   // (not zero: an infinity stays one)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] *= f;
-            }
-            e = now;
-        } else {   // too small to count, but for infinities and NaN
-#pragma unroll
-            for (int i = 0; i < 8; ++i) op[b][0][i] = finite((float)op[b][0][i]) ? (_Float16)0.0f : op[b][0][i];
-            op[b][1] = half8{};
-        }
+        const float unit = __uint_as_float((uint32_t)exponent[b] << 23);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             typedef short s4 __attribute__((ext_vector_type(4)));
@@ -1103,8 +1077,9 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(OD
             half8 v;
             __builtin_memcpy(&v, &lo, 8);
             __builtin_memcpy((char*)&v + 8, &hi, 8);
-            acc[j] = mfma(v, op[b][0], acc[j]);
-            acc[j] = mfma(v, op[b][1], acc[j]);
+            const float4v part = mfma(v, op[b][1], mfma(v, op[b][0], float4v{}));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[j][i] = __builtin_fmaf(part[i], unit, acc[j][i]);
         }
     };
     load_operand(0, 0);
@@ -1114,13 +1089,12 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(OD
         step(std::integral_constant<int, 0>{}, k);
         step(std::integral_constant<int, 1>{}, k + 1);
     }
-    const float up = e > -200 ? power_of_two(e) : 0.0f;
     __syncthreads();
     auto* const sum = (float(*)[8][4][kWave])lds;   // [wave][j][i][lane (n, q)] = feature 16 j + 4 q + i, rank n
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[wave][j][i][lane] = acc[j][i] * up;
+        for (int i = 0; i < 4; ++i) sum[wave][j][i][lane] = acc[j][i];
     __syncthreads();
     float* const out = job.parts > 1 ? side.partial + (job.partial + (int64_t)split * rank_all) * F : result;
     const bool add = a.accumulate && job.parts == 1;

@@ -125,3 +125,30 @@ def test_infinite_operands_of_the_gradients(bd, T, at, rank):
     bd.lora_multitenant_backward(dy, x, None, table, [0] * T, bd.LoraGrads(table, da, [None]), want_dx=False)
     g = float(scale[0]) * (dy.double() @ b[0].double())
     _same_as_formula(da[0], g.t() @ x.double(), "dA")
+
+
+@pytest.mark.parametrize("T", [20, 300, 3000])
+@pytest.mark.parametrize("ranks", [[8], [16, 40], [64, 5, 130]])
+@pytest.mark.parametrize("stride", [1, 3])
+def test_ranks_of_very_different_size(bd, T, ranks, stride):
+    """Every row of dA and column of dB by its own size: ranks up to 2^-30 of the strongest one in g, up to 2^-60 in h.  A value of g or h is kept to
+    2^-22 of itself (two of the sums' 2^-23), or to 2^-38 of its rank's largest; the rest as in lora_ref."""
+    print(f"ranks of very different size T={T} ranks={ranks}", flush=True)
+    out, inn, n = 200, 96, len(ranks)
+    a, b, scale, x, dy = ref64.make(ranks, out, inn, T, seed=T + n)
+    b = [(t.float() * 2.0 ** (10 - 10 * (torch.arange(t.shape[1], device=DEV) % 4))).half() for t in b]
+    h = torch.randn((T, max(ranks)), generator=torch.Generator().manual_seed(4)).to(DEV)
+    h = h * 2.0 ** (20 - 20.0 * (torch.arange(max(ranks), device=DEV) % 4))
+    tok = [(stride * t) % n for t in range(T)]
+    table = bd.LoraTable(a, b, scale)
+    da, db = _gradients(ranks, out, inn)
+    bd.lora_multitenant_backward(dy, x, h, table, tok, bd.LoraGrads(table, da, db), want_dx=False)
+    for e in sorted(set(tok)):
+        r = ranks[e]
+        rows = ref64.rows_of(tok, e, DEV)
+        d, X, H, B, s = dy[rows].double(), x[rows].double(), h[rows, :r].double(), b[e].double(), float(scale[e])
+        g, g_size, adds = s * (d @ B), abs(s) * (d.abs() @ B.abs()), len(rows) / 4 + 32
+        bound = (out / 8 + 16 + adds) * ref64.U32 * (g_size.t() @ X.abs()) + 2.0 ** -38 * g.abs().amax(0)[:, None] * X.abs().sum(0)[None, :]
+        ref64.check(da[e], g.t() @ X, bound, f"dA of tenant {e}")
+        bound = adds * ref64.U32 * abs(s) * (d.abs().t() @ H.abs()) + 2.0 ** -38 * abs(s) * H.abs().amax(0)[None, :] * d.abs().sum(0)[:, None]
+        ref64.check(db[e], s * (d.t() @ H), bound, f"dB of tenant {e}")
