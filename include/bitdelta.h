@@ -437,7 +437,8 @@ bd_status bd_linear_multitenant_tiled_group_q8(int32_t n_mats, const uint16_t* x
  *     h[t] = A_e x[t]                                  e = tenant_of_token[t]
  *     y[t] = fp16( f32(y0[t]) + s_e * (B_e h[t]) )     one rounding; sums in binary32
  * A value of h (of g below) that goes into a matrix-core product keeps 22 bits, or of a value that is far smaller what lies above 2^-39
- * of the largest of its GROUP (and above 2^-125): a token's ranks for y and dx, 32 tokens of one rank for dB and dA.
+ * of the largest of its GROUP (and above 2^-125): a token's ranks for y and dx, 32 tokens of one rank for dB and dA.  Infinities come
+ * out as the formulas have them, but as NaN where one meets a value that is below 2^-37 of its group's largest.
  *   x_f16            [T, in]
  *   a_by_tenant, b_by_tenant   HOST arrays of n_tenants DEVICE pointers; NULL allowed for tenants without a token and where
  *                    the rank is 0

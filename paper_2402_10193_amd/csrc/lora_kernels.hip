@@ -6,7 +6,7 @@
 //
 // The ranks are a few to a few dozen, so that every product here is bound by the activations it streams (x, dy, y0, y) or, in
 // a decode step, by latency; the matrix cores have room to spare.  That room buys precision: h and g are held in binary32 and
-// enter the matrix cores as two binary16 numbers each, hi = fp16(v 2^-e) and lo = fp16(v 2^-e - hi), some 22 bits together.  e
+// enter the matrix cores as two binary16 numbers each, hi = fp16(v 2^-e), toward zero, and lo = fp16(v 2^-e - hi), 22 bits together.  e
 // brings the largest of a token's values (grad: of a rank's values in 32 tokens) to 2^14 .. 2^15, so that neither part leaves the
 // range of binary16 whatever the scale of the activations or of the loss: a value keeps 22 bits, or what lies above 2^-39 of the
 // largest of those it is added up with.  x, dy, A and B are binary16 as they are, the sums binary32.
@@ -81,11 +81,18 @@ __device__ __forceinline__ int group_exponent(float m) {
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
-// hi and lo of v 2^-e (scale = 2^-e); an infinity or NaN goes through in hi alone
+// hi and lo of v 2^-e (scale = 2^-e), both of v's sign and neither zero (down to 2^-37 of the group's largest), so that times an infinity
+// they add up to one; of what is not finite both are v.
 __device__ __forceinline__ void split_half(float v, float scale, _Float16* hi, _Float16* lo) {
     const float s = v * scale;
-    *hi = (_Float16)s;
-    *lo = finite(s) ? (_Float16)(s - (float)*hi) : (_Float16)0.0f;
+    const uint16_t toward_zero = (uint16_t)__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(s, 0.0f));
+    _Float16 h = __builtin_bit_cast(_Float16, toward_zero), l = (_Float16)(s - (float)h);
+    if (l == (_Float16)0.0f) {   // (s is as good as a binary16 number: the one before it, and the step between them)
+        h = __builtin_bit_cast(_Float16, (uint16_t)(toward_zero - ((toward_zero & 0x7fffu) > 0 ? 1 : 0)));
+        l = (_Float16)(s - (float)h);
+    }
+    *hi = h;
+    *lo = finite(s) ? l : h;
 }
 
 // What a workgroup works on.

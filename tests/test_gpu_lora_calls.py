@@ -152,3 +152,37 @@ def test_ranks_of_very_different_size(bd, T, ranks, stride):
         ref64.check(da[e], g.t() @ X, bound, f"dA of tenant {e}")
         bound = adds * ref64.U32 * abs(s) * (d.abs().t() @ H.abs()) + 2.0 ** -38 * abs(s) * H.abs().amax(0)[None, :] * d.abs().sum(0)[:, None]
         ref64.check(db[e], s * (d.t() @ H), bound, f"dB of tenant {e}")
+
+
+@pytest.mark.parametrize("T", [1, 2, 3, 40, 600])
+@pytest.mark.parametrize("rank", [5, 8, 20, 61])
+def test_infinite_inputs_give_what_the_formula_gives(bd, T, rank):
+    """An infinity of A, B, x or dy meets finite values of both signs, some of them whole binary16 numbers: infinities with the formula's sign, by
+    one launch, by tiles of 16 tokens and of 64, forward and backward."""
+    print(f"infinite inputs T={T} rank={rank}", flush=True)
+    out, inn, inf = 200, 160, float("inf")
+    a, b, scale, x, dy = ref64.make([rank], out, inn, T, seed=rank + T)
+    x[:, 1:] = 0                                         # h and g are products of two binary16 numbers, some of one
+    x[::2, 0], a[0][::2, 0] = 1.0, 0.5
+    a[0][a[0] == 0] = 0.25
+    tok, s = [0] * T, float(scale[0])
+    h = x.double() @ a[0].double().t()
+    bad = b[0].clone()
+    bad[130, rank - 1], bad[7, 0] = inf, -inf
+    y = bd.lora_multitenant(x, bd.LoraTable(a, [bad], scale), tok, out=out)
+    _same_as_formula(y, s * (h @ bad.double().t()), "y")
+    g = s * (dy.double() @ b[0].double())
+    bad = a[0].clone()
+    bad[rank - 1, 130], bad[0, 7] = -inf, inf
+    dx = bd.lora_multitenant_backward(dy, None, None, bd.LoraTable([bad], b, scale), tok, None)
+    _same_as_formula(dx, g @ bad.double(), "dx")
+    table = bd.LoraTable(a, b, scale)
+    da, db = _gradients([rank], out, inn)
+    bad = x.clone()
+    bad[T - 1, 11], bad[0, 150] = inf, -inf
+    bd.lora_multitenant_backward(dy, bad, None, table, tok, bd.LoraGrads(table, da, [None]), want_dx=False)
+    _same_as_formula(da[0], g.t() @ bad.double(), "dA")
+    bad = dy.clone()
+    bad[T - 1, 199], bad[0, 100] = inf, -inf
+    bd.lora_multitenant_backward(bad, None, h.float(), table, tok, bd.LoraGrads(table, [None], db), want_dx=False)
+    _same_as_formula(db[0], s * (bad.double().t() @ h), "dB")
