@@ -945,6 +945,7 @@ class LoraTable:
         if self.scale.numel() != len(self.a):
             raise ValueError("one scale per tenant")
         self.n_tenants, self.device = len(self.a), self.scale.get_device()
+        self.streams = _streams_of(self.scale)
 
 
 class LoraGroup:
@@ -966,7 +967,7 @@ class LoraGroup:
         self.a_ptrs = (ctypes.c_void_p * size)(*flat(lambda t: t.a_ptrs))
         self.b_ptrs = (ctypes.c_void_p * size)(*flat(lambda t: t.b_ptrs))
         self.rank_arr = (ctypes.c_int32 * size)(*flat(lambda t: t.rank_arr))
-        self.scales, self.array = [t.scale for t in self.tables], ctypes.c_void_p * self.n
+        self.scales, self.array, self.streams = [t.scale for t in self.tables], ctypes.c_void_p * self.n, set()
         self.device = self.tables[0].device if len({t.device for t in self.tables}) == 1 else None
         self.scale = self.array(*[_ptr(t) or None for t in self.scales])
         self.out_arr = (ctypes.c_int64 * self.n)(*self.outs)
@@ -1003,6 +1004,21 @@ def _memory_of(stream, dev: int):
         return
     with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=dev)):
         yield
+
+
+def _streams_of(t: torch.Tensor) -> set:
+    """The streams that the allocator knows to use memory that has just been made: the current one's."""
+    return {int(torch.cuda.current_stream(t.device).cuda_stream)}
+
+
+def _used_on(owner, tensors, raw: int, stream, dev) -> None:
+    """A call on stream `raw` reads tensors that `owner` keeps and its user does not see: the allocator must not hand them on before that stream is
+    done with them, also where the owner is dropped right after the call."""
+    s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.current_stream(dev) if stream is None else torch.cuda.ExternalStream(int(stream), device=dev)
+    for t in tensors:
+        if t is not None and t.numel() > 0:
+            t.record_stream(s)
+    owner.streams.add(raw)
 
 
 def _stream_of(stream, dev: int) -> int:
@@ -1042,10 +1058,13 @@ def lora_multitenant(x: torch.Tensor, adapters: LoraTable, tenant_of_token, y0: 
     h_ld = _lora_h(h, T)
     if h is not None or workspace.get_device() != dev or adapters.device != dev:
         _here(h, workspace, adapters.scale)
+    raw = _stream_of(stream, dev)
+    if raw not in adapters.streams:
+        _used_on(adapters, (adapters.scale,), raw, stream, dev)
     tok, keep = _tok_pointer(tenant_of_token, T)
     _check(lib().bd_lora_multitenant(x.data_ptr(), adapters.a_ptrs, adapters.b_ptrs, adapters.rank_arr, adapters.scale.data_ptr(), tok,
                                      _arg(y0, torch.float16, (T, out), dev, "y0"), _arg(y, torch.float16, (T, out), dev, "y"), _ptr(h), h_ld,
-                                     T, out, inn, adapters.n_tenants, workspace.data_ptr(), workspace.numel(), _stream_of(stream, dev)),
+                                     T, out, inn, adapters.n_tenants, workspace.data_ptr(), workspace.numel(), raw),
            "bd_lora_multitenant")
     return y
 
@@ -1077,10 +1096,16 @@ def lora_multitenant_group(x: torch.Tensor, group: LoraGroup, tenant_of_token, y
         h_ptrs, h_ld = array(*[_ptr(h) or None for h in hs]), widths.pop()
     if workspace.get_device() != dev or group.device != dev:
         _here(workspace, *group.scales)
+    raw = _stream_of(stream, dev)
+    if raw not in group.streams:
+        for table in group.tables:
+            if raw not in table.streams:
+                _used_on(table, (table.scale,), raw, stream, dev)
+        group.streams.add(raw)
     tok, keep = _tok_pointer(tenant_of_token, T)
     _check(lib().bd_lora_multitenant_group(group.n, x.data_ptr(), group.a_ptrs, group.b_ptrs, group.rank_arr, group.scale, tok, y0_ptrs,
                                            y_ptrs, h_ptrs, h_ld, T, group.out_arr, inn, group.n_tenants, workspace.data_ptr(),
-                                           workspace.numel(), _stream_of(stream, dev)),
+                                           workspace.numel(), raw),
            "bd_lora_multitenant_group")
     return list(ys)
 
@@ -1129,11 +1154,14 @@ def lora_multitenant_backward(dy: torch.Tensor, x: Optional[torch.Tensor], h: Op
     h_ld = _lora_h(h, T)
     if h is not None or workspace.get_device() != dev or adapters.device != dev:
         _here(h, workspace, adapters.scale)
+    raw = _stream_of(stream, dev)
+    if raw not in adapters.streams:
+        _used_on(adapters, (adapters.scale,), raw, stream, dev)
     tok, keep = _tok_pointer(tenant_of_token, T)
     _check(lib().bd_lora_multitenant_backward(dy.data_ptr(), x_ptr, _ptr(h), h_ld, adapters.a_ptrs, adapters.b_ptrs, adapters.rank_arr,
                                               adapters.scale.data_ptr(), tok, dx0_ptr, dx_ptr, grads.da_ptrs if grads else None,
                                               grads.db_ptrs if grads else None, int(accumulate), T, out, inn, adapters.n_tenants,
-                                              workspace.data_ptr(), workspace.numel(), _stream_of(stream, dev)), "bd_lora_multitenant_backward")
+                                              workspace.data_ptr(), workspace.numel(), raw), "bd_lora_multitenant_backward")
     return dx
 
 
@@ -1181,6 +1209,7 @@ class AdamWGroup:
                                    ptrs(lists[2]), ptrs(lists[3]), ptrs(lists[5]) if bits8 else None, ptrs(lists[6]) if bits8 else None,
                                    numel), "bd_adamw_plan")
         self.plan_device = torch.frombuffer(self.plan, dtype=torch.uint8).to(self.device) if n else None
+        self.streams = _streams_of(self.plan_device) if n else set()
 
 
 def adamw(group: AdamWGroup, lr: torch.Tensor, step: torch.Tensor, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
@@ -1193,8 +1222,11 @@ def adamw(group: AdamWGroup, lr: torch.Tensor, step: torch.Tensor, beta1: float 
             raise ValueError(f"{what} is one number")
     if group.n:
         _here(lr, step, grad_scale, skip, group.keep[0][0])
+    raw = _stream(stream)
+    if group.n and raw not in group.streams:
+        _used_on(group, (group.plan_device,), raw, stream, group.device)
     _check(lib().bd_adamw(group.plan, group.bytes, _ptr(group.plan_device), _ptr(lr), _ptr(step), _ptr(grad_scale), _ptr(skip), beta1, beta2, eps, weight_decay,
-                          _stream(stream)), "bd_adamw")
+                          raw), "bd_adamw")
 
 
 def adamw_values(codes: torch.Tensor, second: bool, values: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
