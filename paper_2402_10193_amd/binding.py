@@ -930,6 +930,8 @@ class LoraTable:
                 shapes.add((b.shape[0], a.shape[1]))
         if len(shapes) > 1:
             raise ValueError("the adapters of one matrix have the same out and in")
+        if len({t.device for t in self.a + self.b if t is not None}) > 1:
+            raise ValueError("the adapters of one matrix are on one device")
         self.shape = shapes.pop() if shapes else None   # (out, in)
         self.ranks = [0 if a is None else int(a.shape[0]) for a in self.a]
         self.max_rank = max(self.ranks, default=0)
@@ -1124,6 +1126,8 @@ class LoraGrads:
                     _dev(g, torch.float32, what)
                     if w is None or g.numel() != w.numel():
                         raise ValueError(f"{what} has the elements of its matrix")
+                    if g.device != w.device:
+                        raise ValueError(f"{what} is on {g.device}, its matrix on {w.device}")
         n = max(adapters.n_tenants, 1)
         self.da_ptrs = (ctypes.c_void_p * n)(*[_ptr(g) or None for g in self.da])
         self.db_ptrs = (ctypes.c_void_p * n)(*[_ptr(g) or None for g in self.db])
