@@ -279,7 +279,7 @@ __global__ __launch_bounds__(kDecodeThreads) void lora_decode_kernel(const LoraD
         if (t < count && r < rank) a.h_out[mat][(int64_t)k.col[t] * a.h_ld + r] = h[t][r];
     }
     if (!work) return;
-    const float scale = rank > 0 ? a.scale[mat][k.tenant] : -0.0f;   // (y0 + 0 * -0 is y0, also where it is -0)
+    const float scale = rank > 0 ? a.scale[mat][k.tenant] : 0.0f;
     float sum[kFeatures][TOK] = {};
 #pragma unroll
     for (int o = 0; o < kOctets; ++o)
@@ -299,7 +299,8 @@ __global__ __launch_bounds__(kDecodeThreads) void lora_decode_kernel(const LoraD
         const int64_t f = base + i * kDecodeThreads + threadIdx.x;
 #pragma unroll
         for (int t = 0; t < TOK; ++t)
-            if (f < F && t < count) *(_Float16*)(a.y[mat] + token[t] * F + f) = (_Float16)__builtin_fmaf(sum[i][t], scale, (float)before[i][t]);
+            if (f < F && t < count)   // (without an adapter every bit of y0, of zeros and NaN too)
+                *(_Float16*)(a.y[mat] + token[t] * F + f) = rank > 0 ? (_Float16)__builtin_fmaf(sum[i][t], scale, (float)before[i][t]) : before[i][t];
     }
 }
 
@@ -535,8 +536,7 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
     // read element by element
     const int64_t f0 = ((int64_t)blockIdx.y * kLoraExpandWaves + wave) * kLoraFeatures, base = min(f0, max(F - kLoraFeatures, (int64_t)0)), f = base + 8 * m;
     const bool active = f0 < F, vectors = ROWS != kShortRows || F >= kLoraFeatures;
-    // (y0 + 0 * -0 is y0, also where it is -0; a matrix without outputs, whose h alone is asked for, may have no scales)
-    const float scale = u.rank == 0 ? -0.0f : TR || F == 0 ? 1.0f : a.scale[u.mat][u.tenant];
+    const float scale = TR || u.rank == 0 || F == 0 ? 1.0f : a.scale[u.mat][u.tenant];   // (a matrix whose h alone is asked for may have none)
 
     int64_t at[4];   // where the lane's results belong: token 4 g + i
     half8 before[4];
@@ -681,6 +681,7 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
         half8 v;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = (_Float16)__builtin_fmaf(acc[j][i], up, (float)before[i][j]);
+        if (u.rank == 0) v = before[i];   // every bit of y0, of zeros and NaN too
         if (f >= f0 && F - f >= 8) {
             __builtin_memcpy(y + at[i], &v, 16);
         } else {
@@ -716,8 +717,7 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     // Features f0 .. f0 + 127; a row's last 128 end with it, and of them only those from f0 on are kept.  A row below 128 is read element
     // by element.
     int64_t f0 = (int64_t)blockIdx.y * kLoraFeatures;
-    // (y0 + 0 * -0 is y0, also where it is -0; a matrix without outputs, whose h alone is asked for, may have no scales)
-    const float scale = u.rank == 0 ? -0.0f : TR || F == 0 ? 1.0f : a.scale[u.mat][u.tenant];
+    const float scale = TR || u.rank == 0 || F == 0 ? 1.0f : a.scale[u.mat][u.tenant];   // (a matrix whose h alone is asked for may have none)
     const bool vectors = ROWS != kShortRows || F >= kLoraFeatures;
     auto begin_of = [&](int64_t first) { return min(first, max(F - kLoraFeatures, (int64_t)0)); };
 
@@ -907,6 +907,10 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = (_Float16)__builtin_fmaf(acc[j][i], up[i], y0 ? (float)before[i][j] : 0.0f);
+        if (u.rank == 0 && y0) {   // every bit of y0, of zeros and NaN too
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = before[i];
+        }
         // the next y0 is asked for before the stores: no wait for it has to wait for them (past the end: the last features' once more)
         load_y0(before, begin_of(min(f0 + stride, F - 1)));
 #pragma unroll

@@ -186,3 +186,19 @@ def test_infinite_inputs_give_what_the_formula_gives(bd, T, rank):
     bad[T - 1, 199], bad[0, 100] = inf, -inf
     bd.lora_multitenant_backward(bad, None, h.float(), table, tok, bd.LoraGrads(table, [None], db), want_dx=False)
     _same_as_formula(db[0], s * (bad.double().t() @ h), "dB")
+
+
+@pytest.mark.parametrize("T", [2, 40, 600])
+@pytest.mark.parametrize("out", [5, 136])
+def test_every_bit_of_tokens_without_an_adapter(bd, T, out):
+    """All 65536 binary16 patterns among them, NaN of every kind, in y and in dx; the other tenant's tokens take part."""
+    inn = 64
+    a, b, scale, x, dy = ref64.make([8, 0], out, inn, T, seed=T)
+    table, tok = bd.LoraTable(a, b, scale), [t % 2 for t in range(T)]
+    for first in range(0, 65536, (T + 1) // 2 * out) if T > 2 else (0x0000, 0x7BFD, 0x7C00, 0x7D00, 0x7E01, 0xFBFF, 0xFC01, 0xFE55):
+        y0 = ((torch.arange(T * out, device=DEV) + first) & 0xFFFF).to(torch.int32).to(torch.int16).view(torch.float16).view(T, out)
+        y = bd.lora_multitenant(x, table, tok, y0=y0)
+        assert torch.equal(y[1::2].view(torch.int16), y0[1::2].view(torch.int16)), f"y from {first:#x}"
+    dx0 = torch.full((T, inn), 0x7C01, dtype=torch.int16, device=DEV).view(torch.float16)
+    dx = bd.lora_multitenant_backward(dy, None, None, table, tok, None, dx0=dx0)
+    assert torch.equal(dx[1::2].view(torch.int16), dx0[1::2].view(torch.int16))
