@@ -717,7 +717,7 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     // Features f0 .. f0 + 127; a row's last 128 end with it, and of them only those from f0 on are kept.  A row below 128 is read element
     // by element.
     int64_t f0 = (int64_t)blockIdx.y * kLoraFeatures;
-    const float scale = TR || u.rank == 0 || F == 0 ? 1.0f : a.scale[u.mat][u.tenant];   // (a matrix whose h alone is asked for may have none)
+    const float scale = TR || F == 0 ? 1.0f : a.scale[u.mat][u.tenant];   // (a matrix whose h alone is asked for may have none)
     const bool vectors = ROWS != kShortRows || F >= kLoraFeatures;
     auto begin_of = [&](int64_t first) { return min(first, max(F - kLoraFeatures, (int64_t)0)); };
 
@@ -748,6 +748,30 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
             for (int i = 0; i < 4; ++i) to[i] = half8{};
         }
     };
+    uint16_t* const y = a.y[u.mat];
+    auto store_y = [&](const half8 (&v)[4], int64_t f) {   // at the features f .. f + 127, those before f0 left out
+        const int64_t fl = f + 8 * m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (16 * wave + 4 * g + i >= u.count) continue;
+            if (fl >= f0 && F - fl >= 8) {
+                __builtin_memcpy(y + row[i] + f, &v[i], 16);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (fl + j >= f0 && fl + j < F) *(_Float16*)(y + row[i] + f + j) = v[i][j];
+            }
+        }
+    };
+    if (u.rank == 0) {   // every bit of y0, of zeros and NaN too
+        for (; f0 < F; f0 += stride) {
+            load_y0(before, begin_of(f0));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) before[i] = y0 ? before[i] : half8{};
+            store_y(before, begin_of(f0));
+        }
+        return;
+    }
     // the thread's 16 bytes of the weights
     const int piece_row = TR ? (int)threadIdx.x >> 4 : (int)threadIdx.x >> 1, piece_col = TR ? 8 * ((int)threadIdx.x & 15) : 8 * ((int)threadIdx.x & 1);
     char* const piece_at = pieces + (TR ? piece_row * 272 + piece_col * 2 : piece_row * 32 + piece_col * 2 + (piece_row >> 3) * 16);
@@ -788,12 +812,10 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
     half8 piece0[RS] = {};
     int left0[RS] = {};
     if (work) {
-        if (padded > 0) {   // two pieces before h: nothing is in flight when the turns begin
-            next_piece();
+        next_piece();   // two pieces before h: nothing is in flight when the turns begin
 #pragma unroll
-            for (int k = 0; k < RS; ++k) piece0[k] = piece[k], left0[k] = piece_left[k];
-            next_piece();
-        }
+        for (int k = 0; k < RS; ++k) piece0[k] = piece[k], left0[k] = piece_left[k];
+        next_piece();
         load_y0(before, begin_of(f0));
     }
 
@@ -865,17 +887,16 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
         }
     }
     if (!work) return;   // (of the whole workgroup)
-    if (padded > 0) put_piece(0, piece0, left0);
+    put_piece(0, piece0, left0);
     __syncthreads();
 
-    uint16_t* const y = a.y[u.mat];
     const _Float16* const mine = (g < 2 ? hi : lo) + (16 * wave + m) * pitch + 8 * (g & 1);
     float up[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) up[i] = unit[16 * wave + 4 * g + i];
     int buffer = 0;
     for (; f0 < F; f0 += stride) {
-        const int64_t f = begin_of(f0), fl = f + 8 * m;
+        const int64_t f = begin_of(f0);
         float4v acc[8] = {};
         auto step = [&](int r) {
             put_piece(buffer ^ 1, piece, piece_left);   // of the next ranks or features
@@ -900,30 +921,16 @@ __global__ __launch_bounds__(kExpandThreads, ROWS == kShortRows ? 2 : 3) void lo
             buffer ^= 1;
             __syncthreads();
         };
-        if (padded > 0) step(0);   // (not in the loop: what is in flight is known at each of its waits)
+        step(0);   // (not in the loop: what is in flight is known at each of its waits)
         for (int r = 16 * RS; r < padded; r += 16 * RS) step(r);
         half8 v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = (_Float16)__builtin_fmaf(acc[j][i], up[i], y0 ? (float)before[i][j] : 0.0f);
-        if (u.rank == 0 && y0) {   // every bit of y0, of zeros and NaN too
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = before[i];
-        }
         // the next y0 is asked for before the stores: no wait for it has to wait for them (past the end: the last features' once more)
         load_y0(before, begin_of(min(f0 + stride, F - 1)));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (16 * wave + 4 * g + i >= u.count) continue;
-            if (fl >= f0 && F - fl >= 8) {
-                __builtin_memcpy(y + row[i] + f, &v[i], 16);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (fl + j >= f0 && fl + j < F) *(_Float16*)(y + row[i] + f + j) = v[i][j];
-            }
-        }
+        store_y(v, f);
     }
 }
 
