@@ -508,6 +508,8 @@ bd_status bd_lora_multitenant_backward(const uint16_t* dy_f16, const uint16_t* x
  * Tensors 16-byte aligned, scales 4.  Nothing may overlap anything else (BD_ERR_ALIAS): no tensor twice.
  * States in 8 bits: a byte's value is V times its block's scale, V = f where the exponent bits e are 0, else (2^F + f) 2^(e-1).
  *     m: bit 7 the sign, bits 6-4 e, bits 3-0 f (F = 4); m = +-scale V, rounded to nearest even; scale = max |m| / 1984
+ *        (a gradient that does not change at all stops m within half a code step / (1 - beta1) of it, some 16 to 31 % of m at 0.9;
+ *        noise carries it on)
  *     v: bits 7-5 e, bits 4-0 f (F = 5); sqrt(v) = scale V; scale = sqrt(max v) / 4032; rounded up with the probability of its
  *        fraction of a code step, by a hash of (index in the tensor, step), never to zero where v is not
  *   The update itself uses m and v before they are rounded.  All zeros (bytes and scales) is the state before the first step.  A

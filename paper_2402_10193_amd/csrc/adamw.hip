@@ -4,8 +4,8 @@
 //   p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps);   p16 = fp16(p)
 //
 // Bound: HBM.  An element costs 28 bytes with binary32 states and gradients (30 with the binary16 copy), 16.06 (18.06) with 8-bit states.
-// The seven matrices of a layer, 4096 and 11008 wide, 202 million elements, fp16 gradients and copies (5.67 GB): 1058 us, 5.4 TB/s; 8-bit states,
-// binary32 gradients (3.66 GB): 670 us, 5.5 TB/s; 16 tenants' adapters of rank 13, 224 tensors of 53248 and 143104 elements, 8-bit (293 MB):
+// The seven matrices of a layer, 4096 and 11008 wide, 202 million elements, fp16 gradients and copies (5.67 GB): 1060 us, 5.3 TB/s; 8-bit states,
+// binary32 gradients (3.66 GB): 685 us, 5.3 TB/s; 16 tenants' adapters of rank 13, 224 tensors of 53248 and 143104 elements, 8-bit (293 MB):
 // 62 us, 4.7 TB/s.  A plain copy of 1 GiB moves 5.2 TB/s.
 //
 // 8-bit states: 256 neighbours of a tensor, what a wavefront handles per step, share one binary32 scale each for m and v, found
@@ -13,7 +13,8 @@
 // integer V: 3 exponent bits e and F fraction bits f, V = f for e = 0, else (2^F + f) 2^(e - 1).
 //   m  sign and F = 4:  m = +-scale V,        scale = max |m| / 1984          (steps of 3 to 6 %, range 1 : 1984)
 //   v  F = 5:           sqrt(v) = scale V,    scale = sqrt(max v) / 4032      (steps of 1.6 to 3 %, range of v 1 : 1.6e7)
-// m is rounded to nearest (even).  v moves by little: b2 = 0.999 changes sqrt(v) by 0.05 % a step, a thirtieth of a code step, and
+// m is rounded to nearest (even): beside gradients that do not change at all it stops within half a code step / (1 - b1) of them, some 16 to 31 % of m
+// for b1 = 0.9; noise of a third of a gradient's size brings it to 1 % on average.  v moves by little: b2 = 0.999 changes sqrt(v) by 0.05 % a step, a thirtieth of a code step, and
 // nearest rounding would hold it where it is (with gradients of constant size at a 25th of g^2, so steps five times too
 // long).  It is rounded up with the probability of its fraction of a code step, from a hash of the element's index and the
 // number of the step: right on average, and the same bits for the same inputs.  A v that is not zero does not become zero,

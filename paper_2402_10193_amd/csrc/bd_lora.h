@@ -152,7 +152,8 @@ struct LoraReduceArgs {
     struct { float* out; const float* partial; int64_t n; int32_t parts; } job[kLoraRecords];
 };
 
-// workgroups of the shrink for one tile and part of the sum
+// Workgroups of the shrink for one tile and part of the sum.  (The backward kernel of ranks that are no multiple of 8 takes 16 ranks each; how its sum
+// is cut goes by this all the same.)
 constexpr int lora_shrink_groups(int rank, int columns) { return (rank + 15) / 16 <= 1 || columns == 16 ? (rank + 15) / 16 : (rank + 63) / 64; }
 
 // `columns`: tokens of a tile (16: records are tiles; else records are jobs, 64).  max_rank: the largest rank of the records;

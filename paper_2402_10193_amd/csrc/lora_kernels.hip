@@ -698,7 +698,7 @@ __global__ __launch_bounds__(kExpandThreads) void lora_expand_few_kernel(const L
 // behind a row), where every wavefront reads them into matrix-core order without bank conflicts: read from memory in that order,
 // neighbouring lanes would be rows apart and an instruction would take the address unit four times as long.  While a piece is used the
 // next but one is on its way, and the next features' y0.
-// Bound by y0 and y: 4096 tokens by 11008, rank 16 (180 MB) 43 us, 4.2 TB/s; 8192 by 4096, rank 64 (134 MB) 38 us, 3.5 TB/s (a barrier for every
+// Bound by y0 and y: 4096 tokens by 11008, rank 16 (180 MB) 42 us, 4.3 TB/s; 8192 by 4096, rank 64 (134 MB) 39 us, 3.4 TB/s (a barrier for every
 // 16 ranks instead of 32: 42.9 us).  Features in turn, not next to each other, for a workgroup: 43 us, else 47.
 constexpr int kPieces = 128 * 32 + 16 * 16;
 template <bool TR, int ROWS, int RS>   // RS: times 16 ranks at a time
@@ -1018,7 +1018,7 @@ constexpr int kGradPitch = 128 + 16;   // halves: 4 rows apart on banks of their
 // and then go into the sum, whatever the sizes of the tiles before.
 // Loads are never under a condition (past the end they repeat the last tile's), or the wait for them would be for all.
 // Bound by the streams of x and dy: 4096 tokens of 8 tenants, 4096 -> 4096, rank 16 (67 MB) 22 us, 3.0 TB/s; 8192 of 2, 4096 -> 11008, rank 64
-// (247 MB) 66 us, 3.7 TB/s.
+// (247 MB) 68 us, 3.6 TB/s.
 template <int RW, bool ODD>
 __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(ODD ? 2 : 3, 3))) void lora_grad_kernel(const LoraGradArgs a) {
     constexpr int TW = kLoraGradWaves / RW, N = 8 / RW, kBuffers = RW > 1 ? 2 : 1;   // groups; rows of 4 per wavefront and tile
